@@ -534,6 +534,93 @@ int rov_block_forward_static(const rov_block_weights *w, const void *x, void *y,
                              int mask_ready, uint64_t *mask, uint64_t *next_mask,
                              void *main_stream, void *side_stream);
 
+/* ---------------------------------------------------------------- rotary positions
+ * Queries and keys turned by their positions, in the forms that the block's own rotary embedding (adjacent pairs,
+ * whole head, plain frequencies) leaves out.  Pair p of a head, (a, b), at position s becomes
+ *     magnitude * (a cos t - b sin t, a sin t + b cos t),   t = s * f_p,   f_p = theta^(-2p/rot),
+ * with the pairs (2p, 2p+1) of the head's first `rot` elements (ROV_ROPE_INTERLEAVED) or (p, p + rot/2)
+ * (ROV_ROPE_HALVES); elements behind `rot` pass unchanged.  For contexts beyond the trained one:
+ *   ROV_ROPE_SCALE_LINEAR  f_p / factor;
+ *   ROV_ROPE_SCALE_PARTS   f_p * (k + (1 - k) / factor), k = clamp((r - turns_low) / (turns_high - turns_low), 0, 1),
+ *                          r = trained_len * f_p / (2 pi): pairs that turn often within the trained length keep
+ *                          their frequency, slow ones are interpolated.
+ * backward != 0 turns by -t with the same magnitude: the gradients of Q and K from those of the results.
+ * Element (b, s, h, e) of Q lives at Q[b*strides[0] + s*strides[1] + h*strides[2] + e], of Qo with strides[3..5], of
+ * K with strides[6..8], of Ko with strides[9..11]; strides in elements, the head dimension is contiguous.
+ * Qo may be Q and Ko may be K (in place, with equal strides, else ROV_ERR_INVALID); otherwise results must not
+ * overlap inputs.  Hkv == 0: no keys (K, Ko ignored).  dtype ROV_F32 or ROV_BF16; arithmetic in fp32.
+ * positions: device, position of token (b, s) at positions[b*positions_stride + s] (stride 0: one row for all
+ * sequences), any value whose angle is below 2^30; NULL: token s is at position s.  Angles are formed in double.
+ * cfg lies in host memory.  rot even, 0 < rot <= d; d > 512: ROV_ERR_UNSUPPORTED. */
+#define ROV_ROPE_INTERLEAVED 0
+#define ROV_ROPE_HALVES 1
+#define ROV_ROPE_SCALE_NONE 0
+#define ROV_ROPE_SCALE_LINEAR 1
+#define ROV_ROPE_SCALE_PARTS 2
+typedef struct rov_rope_cfg {
+    int layout, rot, scaling;
+    int trained_len;            /* PARTS */
+    float theta, factor;        /* factor: LINEAR and PARTS */
+    float turns_low, turns_high; /* PARTS */
+    float magnitude;            /* 1 for none */
+} rov_rope_cfg;
+
+int rov_rope(const rov_rope_cfg *cfg, const void *Q, void *Qo, const void *K, void *Ko, int B, int S, int H,
+             int Hkv, int d, const int64_t strides[12], int dtype, const int64_t *positions,
+             int64_t positions_stride, int backward, void *stream);
+
+/* ---------------------------------------------------------------- norms around a block
+ * The norm behind one block's branch and the norm before the next, with the branch's gate and the residual scale:
+ *     y  = x_scale * x + h_scale * gate * P(h),   P(h) = RMS(h) * w_post, or h without w_post (NULL)
+ *     yn = RMS(y) * w_pre                         (w_pre and yn NULL together: not computed)
+ * RMS(v) = v / sqrt(mean v^2 + eps) over a row of n.  x: the residual stream, h: the branch's output (e.g. the
+ * projection behind attention), both [rows, n]; gate [rows / rows_per_gate, n] (NULL: ones; rows % rows_per_gate == 0),
+ * row r uses gate row r / rows_per_gate; weights [n].  All of dtype ROV_F32 or ROV_BF16, arithmetic and sums in fp32; yn
+ * is formed from y before y is rounded.  yn_fp8_scale > 0 (bf16 only): yn holds OCP e4m3 bytes of
+ * (value / yn_fp8_scale), as the fp8 products take their activations; else 0.
+ * ld: row strides of x, h, y, yn in elements (>= n).  y and yn may be x or h (with the same stride).
+ * n > 32768: ROV_ERR_UNSUPPORTED. */
+int rov_norm_residual(const void *x, const void *h, const void *w_post, const void *gate, const void *w_pre,
+                      void *y, void *yn, int64_t rows, int n, const int64_t ld[4], int64_t rows_per_gate, int dtype,
+                      float x_scale, float h_scale, float eps, float yn_fp8_scale, void *stream);
+
+/* Its gradients.  y: the forward pass's result, h its input; dy, dn: the gradients that reach y (from the residual
+ * stream; NULL: none) and yn (NULL exactly when w_pre is).  dx, dh [rows, n] in dtype; dw_post [n], dgate
+ * [rows / rows_per_gate, n] and dw_pre [n] in fp32, summed in a fixed order.  Results that are NULL are not made; h may
+ * be NULL where neither w_post nor dgate needs it, y without w_pre.  dx and dh may be any of the four inputs (same stride).
+ * ld: row strides of y, h, dy, dn, dx, dh.  workspace: 16-byte aligned device scratch of
+ * rov_norm_residual_bwd_workspace_bytes (0 for invalid arguments), needed for the three sums only. */
+size_t rov_norm_residual_bwd_workspace_bytes(int64_t rows, int n, int64_t rows_per_gate, int dtype);
+int rov_norm_residual_bwd(const void *y, const void *h, const void *w_post, const void *gate, const void *w_pre,
+                          const void *dy, const void *dn, void *dx, void *dh, float *dw_post, float *dgate,
+                          float *dw_pre, int64_t rows, int n, const int64_t ld[6], int64_t rows_per_gate, int dtype,
+                          float x_scale, float h_scale, float eps, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/* ---------------------------------------------------------------- loss over the vocabulary
+ * Softmax cross entropy of the logits z = scale * X W^T, X [M, K] hidden states, W [V, K] output weights, without
+ * keeping z (M x V): the vocabulary is walked in pieces.
+ *     lse[m] = log sum_v exp z[m][v],   loss[m] = lse[m] - z[m][targets[m]],
+ * both fp32 [M], for every row: reductions are the caller's.  targets: int64 [M]; a row whose target is ignore_index (which must
+ * lie outside [0, V)) has loss 0 and no gradient, whatever its X holds; any other target outside [0, V) gives a NaN loss (and NaN gradients).
+ * dtype of X and W: ROV_F32 or ROV_BF16; row strides ldx, ldw >= K in elements.  Logits and sums are fp32.
+ * vocab_piece: columns of a piece (rounded up to 256), 0: chosen by the library; it sets the workspace's size and
+ * does not change what is computed beyond the order of fp32 sums.
+ * workspace: 256-byte aligned device scratch of rov_linear_xent_workspace_bytes (0 for invalid arguments). */
+size_t rov_linear_xent_workspace_bytes(int M, int V, int K, int dtype, int backward, int vocab_piece);
+int rov_linear_xent(const void *X, const void *W, const int64_t *targets, int M, int V, int K, int64_t ldx,
+                    int64_t ldw, int dtype, float scale, int64_t ignore_index, float *loss, float *lse,
+                    int vocab_piece, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its gradients, from the lse of the forward call and the gradients of loss and (may be NULL) lse:
+ *     G = scale * (softmax(z) * (dloss + dlse) - onehot(target) * dloss),   dX = G W,   dW = G^T X,
+ * in the dtype of X and W, row strides lddx, lddw (>= K).  dX or dW may be NULL.  fp32 accumulation; for bf16, G is rounded to bf16 for
+ * the matrix products.  Every element of dX and dW is written.  The logits are made a second time. */
+int rov_linear_xent_bwd(const void *X, const void *W, const int64_t *targets, const float *lse,
+                        const float *dloss, const float *dlse, int M, int V, int K, int64_t ldx, int64_t ldw,
+                        int dtype, float scale, int64_t ignore_index, void *dX, void *dW, int64_t lddx,
+                        int64_t lddw, int vocab_piece, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

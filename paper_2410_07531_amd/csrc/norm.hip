@@ -1,0 +1,533 @@
+// The norms behind one block and before the next (paper Fig. 2's normalisation layers in their RMS form), fused with
+// the branch's gate and the residual scale, forward and backward:
+//     y  = x_scale * x + h_scale * gate * P(h),   P(h) = h / sqrt(mean h^2 + eps) * w_post   (h itself without w_post)
+//     yn = y / sqrt(mean y^2 + eps) * w_pre                                                   (absent without w_pre)
+// and, with dy, dn the gradients of y and yn, r = 1/sqrt(mean + eps), t = w_pre dn, hat = y r:
+//     g  = dy + r (t - hat mean(hat t));  dx = x_scale g;  q = h_scale gate g
+//     dh = r_h (w_post q - h r_h mean(h r_h w_post q));   dw_pre = sum dn hat;  dw_post = sum q h r_h;
+//     dgate = sum over the gate's rows of h_scale g P(h).
+// What bounds both: memory (4 and 6 passes over rows x n).  A workgroup holds a row in registers, so each tensor
+// passes once; all sums are fp32 in a fixed order.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "fp8_device.h"
+#include "rov_internal.h"
+#include "row_device.h"
+
+namespace rov {
+namespace {
+
+constexpr int kMaxRow = 32768;
+
+struct NormParams {
+    const void* x;
+    const void* h;
+    const void* w_post;
+    const void* gate;
+    const void* w_pre;
+    void* y;
+    void* yn;
+    int64_t ld_x, ld_h, ld_y, ld_yn;
+    int rows, n, rows_per_gate;
+    float x_scale, h_scale, eps, inv_n, yn_inv;   // yn_inv: 1 / (scale of the e4m3 result)
+};
+
+template <typename T, int W>
+__device__ __forceinline__ void load_or(const void* base, int at, float (&f)[W], float otherwise) {
+    if (base != nullptr) {
+        Piece<T, W> v;
+        v.load((const T*)base + at);
+        v.get(f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j) f[j] = otherwise;
+    }
+}
+
+// One workgroup of NT threads a row, VPT pieces of W elements a thread.  OUT8: yn is e4m3 bytes.
+template <typename T, int W, int NT, int VPT, bool OUT8>
+__global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormParams p) {
+    __shared__ float red[2][NT / 64];
+    __builtin_amdgcn_s_setprio(3);   // beside a co-resident RNG grid: ahead of its long integer multiplies
+    const int64_t row = blockIdx.x;
+    const T* const x = (const T*)p.x + row * p.ld_x;
+    const T* const h = (const T*)p.h + row * p.ld_h;
+    const T* const gate = p.gate != nullptr ? (const T*)p.gate + (row / p.rows_per_gate) * p.n : nullptr;
+    Piece<T, W> xv[VPT], hv[VPT];
+#pragma unroll
+    for (int c = 0; c < VPT; ++c) {
+        const int e = (c * NT + (int)threadIdx.x) * W;
+        xv[c].zero();
+        hv[c].zero();
+        if (e < p.n) {
+            hv[c].load(h + e);
+            xv[c].load(x + e);
+        }
+    }
+    float inv_h = 1.0f;
+    if (p.w_post != nullptr) {
+        float s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < VPT; ++c) {
+            float f[W];
+            hv[c].get(f);
+#pragma unroll
+            for (int j = 0; j < W; ++j) s = __builtin_fmaf(f[j], f[j], s);
+        }
+        inv_h = 1.0f / sqrtf(workgroup_sum<NT>(s, red[0]) * p.inv_n + p.eps);
+    }
+    float y[VPT][W], s = 0.0f;
+#pragma unroll
+    for (int c = 0; c < VPT; ++c) {
+        const int e = (c * NT + (int)threadIdx.x) * W;
+        float f[W];
+        hv[c].get(f);
+        xv[c].get(y[c]);
+        if (e < p.n) {
+            float wp[W], g[W];
+            load_or<T, W>(p.w_post, e, wp, 1.0f);
+            load_or<T, W>(gate, e, g, 1.0f);
+#pragma unroll
+            for (int j = 0; j < W; ++j) y[c][j] = p.x_scale * y[c][j] + p.h_scale * g[j] * (f[j] * inv_h * wp[j]);
+            Piece<T, W> out;
+            out.set(y[c]);
+            out.store((T*)p.y + row * p.ld_y + e);
+        } else {
+#pragma unroll
+            for (int j = 0; j < W; ++j) y[c][j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) s = __builtin_fmaf(y[c][j], y[c][j], s);
+    }
+    if (p.w_pre == nullptr) return;
+    const float inv_y = 1.0f / sqrtf(workgroup_sum<NT>(s, red[1]) * p.inv_n + p.eps);
+#pragma unroll
+    for (int c = 0; c < VPT; ++c) {
+        const int e = (c * NT + (int)threadIdx.x) * W;
+        if (e >= p.n) continue;
+        float w[W];
+        load_or<T, W>(p.w_pre, e, w, 1.0f);
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j] *= y[c][j] * inv_y;   // (y not yet rounded: yn is one rounding away from the formula)
+        if constexpr (OUT8) {
+            uint8_t* const out = (uint8_t*)p.yn + row * p.ld_yn + e;
+            if constexpr (W == 8) {
+                *reinterpret_cast<uint2*>(out) = make_uint2(
+                    pack_e4m3x4(w[0] * p.yn_inv, w[1] * p.yn_inv, w[2] * p.yn_inv, w[3] * p.yn_inv),
+                    pack_e4m3x4(w[4] * p.yn_inv, w[5] * p.yn_inv, w[6] * p.yn_inv, w[7] * p.yn_inv));
+            } else {
+#pragma unroll
+                for (int j = 0; j < W; ++j) out[j] = (uint8_t)f32_to_e4m3(w[j] * p.yn_inv);
+            }
+        } else {
+            Piece<T, W> out;
+            out.set(w);
+            out.store((T*)p.yn + row * p.ld_yn + e);
+        }
+    }
+}
+
+struct NormBwdParams {
+    const void* y;
+    const void* h;
+    const void* w_post;
+    const void* gate;
+    const void* w_pre;
+    const void* dy;
+    const void* dn;
+    void* dx;
+    void* dh;
+    float* dgate;       // written here only where a workgroup holds whole groups
+    float* part_h;      // [workgroups][n]: sums of g h r_h (times the gate where a workgroup holds whole groups)
+    float* part_y;      // [workgroups][n]: sums of dn y r
+    int64_t ld_y, ld_h, ld_dy, ld_dn, ld_dx, ld_dh;
+    int rows, n, rows_per_gate;
+    int chunks;         // workgroups that share a group (rows of one gate)
+    int groups;
+    float x_scale, h_scale, eps, inv_n;
+};
+
+// A workgroup walks over rows of one group (chunk blockIdx.x % chunks of group blockIdx.x / chunks) or, WHOLE, over
+// whole groups (blockIdx.x, blockIdx.x + gridDim.x, ...), and keeps the column sums of its rows in registers.
+// Row sums: the sum behind dh's mean is linear in g, so its three parts are summed beside mean(y^2), mean(y t) and
+// mean(h^2) and one barrier a row is enough (two sets of scratch by the parity of the row).
+template <typename T, int W, int NT, int VPT, bool WHOLE>
+__global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormBwdParams p) {
+    __shared__ float red[2][6][NT / 64];
+    __builtin_amdgcn_s_setprio(3);
+    float col_h[VPT][W], col_y[VPT][W], col_g[WHOLE ? VPT : 1][W];
+#pragma unroll
+    for (int c = 0; c < VPT; ++c)
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            col_h[c][j] = 0.0f;
+            col_y[c][j] = 0.0f;
+            if constexpr (WHOLE) col_g[c][j] = 0.0f;
+        }
+    const bool has_pre = p.w_pre != nullptr, has_post = p.w_post != nullptr;
+    const bool with_h = p.h != nullptr;
+    int parity = 0;
+    for (int group = WHOLE ? (int)blockIdx.x : (int)blockIdx.x / p.chunks; group < p.groups; group += WHOLE ? (int)gridDim.x : p.groups) {
+        int64_t r0 = (int64_t)group * p.rows_per_gate, r1 = r0 + p.rows_per_gate;
+        if constexpr (!WHOLE) {
+            const int64_t len = p.rows_per_gate, chunk = (int)blockIdx.x % p.chunks;
+            r1 = r0 + len * (chunk + 1) / p.chunks;
+            r0 += len * chunk / p.chunks;
+        }
+        const T* const gate = p.gate != nullptr ? (const T*)p.gate + (int64_t)group * p.n : nullptr;
+        for (int64_t row = r0; row < r1; ++row) {
+            Piece<T, W> yv[VPT], hv[VPT], dyv[VPT], dnv[VPT];
+#pragma unroll
+            for (int c = 0; c < VPT; ++c) {
+                const int e = (c * NT + (int)threadIdx.x) * W;
+                yv[c].zero(); hv[c].zero(); dyv[c].zero(); dnv[c].zero();
+                if (e < p.n) {
+                    if (has_pre) {
+                        yv[c].load((const T*)p.y + row * p.ld_y + e);
+                        dnv[c].load((const T*)p.dn + row * p.ld_dn + e);
+                    }
+                    if (with_h) hv[c].load((const T*)p.h + row * p.ld_h + e);
+                    if (p.dy != nullptr) dyv[c].load((const T*)p.dy + row * p.ld_dy + e);
+                }
+            }
+            float sum[6] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < VPT; ++c) {
+                const int e = (c * NT + (int)threadIdx.x) * W;
+                if (e >= p.n) continue;
+                float y[W], h[W], dy[W], t[W], wp[W], g[W], w[W];
+                yv[c].get(y); hv[c].get(h); dyv[c].get(dy); dnv[c].get(t);
+                load_or<T, W>(p.w_pre, e, w, 0.0f);
+                load_or<T, W>(p.w_post, e, wp, 0.0f);
+                load_or<T, W>(gate, e, g, 1.0f);
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    t[j] *= w[j];
+                    const float u = h[j] * wp[j] * g[j];
+                    sum[0] = __builtin_fmaf(y[j], y[j], sum[0]);
+                    sum[1] = __builtin_fmaf(y[j], t[j], sum[1]);
+                    sum[2] = __builtin_fmaf(h[j], h[j], sum[2]);
+                    sum[3] = __builtin_fmaf(u, dy[j], sum[3]);
+                    sum[4] = __builtin_fmaf(u, t[j], sum[4]);
+                    sum[5] = __builtin_fmaf(u, y[j], sum[5]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+#pragma unroll
+                for (int s = 32; s > 0; s >>= 1) sum[i] += __shfl_xor(sum[i], s);
+            }
+            if constexpr (NT > 64) {
+                if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                    for (int i = 0; i < 6; ++i) red[parity][i][threadIdx.x >> 6] = sum[i];
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 6; ++i) {
+                    sum[i] = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < NT / 64; ++w) sum[i] += red[parity][i][w];
+                }
+                parity ^= 1;
+            }
+            const float r = has_pre ? 1.0f / sqrtf(sum[0] * p.inv_n + p.eps) : 0.0f;
+            const float rh = has_post ? 1.0f / sqrtf(sum[2] * p.inv_n + p.eps) : 1.0f;
+            const float my = r * r * r * sum[1] * p.inv_n;                      // y times this is hat * r * mean(hat t)
+            const float mh = has_post ? rh * rh * rh * p.inv_n * p.h_scale * (sum[3] + r * sum[4] - my * sum[5]) : 0.0f;
+#pragma unroll
+            for (int c = 0; c < VPT; ++c) {
+                const int e = (c * NT + (int)threadIdx.x) * W;
+                if (e >= p.n) continue;
+                float y[W], h[W], dy[W], dn[W], wp[W], g[W], w[W];
+                yv[c].get(y); hv[c].get(h); dyv[c].get(dy); dnv[c].get(dn);
+                load_or<T, W>(p.w_pre, e, w, 0.0f);
+                load_or<T, W>(p.w_post, e, wp, 1.0f);
+                load_or<T, W>(gate, e, g, 1.0f);
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    const float gy = dy[j] + r * w[j] * dn[j] - y[j] * my;
+                    col_y[c][j] = __builtin_fmaf(dn[j] * r, y[j], col_y[c][j]);
+                    col_h[c][j] = __builtin_fmaf(gy * rh, h[j], col_h[c][j]);
+                    dy[j] = p.x_scale * gy;
+                    h[j] = rh * wp[j] * (p.h_scale * g[j] * gy) - h[j] * mh;
+                }
+                Piece<T, W> out;
+                if (p.dx != nullptr) {
+                    out.set(dy);
+                    out.store((T*)p.dx + row * p.ld_dx + e);
+                }
+                if (p.dh != nullptr) {
+                    out.set(h);
+                    out.store((T*)p.dh + row * p.ld_dh + e);
+                }
+            }
+        }
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int c = 0; c < VPT; ++c) {
+                const int e = (c * NT + (int)threadIdx.x) * W;
+                if (e >= p.n) continue;
+                float wp[W], g[W];
+                load_or<T, W>(p.w_post, e, wp, 1.0f);
+                load_or<T, W>(gate, e, g, 1.0f);
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    if (p.dgate != nullptr) p.dgate[(int64_t)group * p.n + e + j] = p.h_scale * wp[j] * col_h[c][j];
+                    col_g[c][j] = __builtin_fmaf(g[j], col_h[c][j], col_g[c][j]);
+                    col_h[c][j] = 0.0f;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < VPT; ++c) {
+        const int e = (c * NT + (int)threadIdx.x) * W;
+        if (e >= p.n) continue;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            if (p.part_h != nullptr) p.part_h[(int64_t)blockIdx.x * p.n + e + j] = WHOLE ? col_g[c][j] : col_h[c][j];
+            if (p.part_y != nullptr) p.part_y[(int64_t)blockIdx.x * p.n + e + j] = col_y[c][j];
+        }
+    }
+}
+
+struct NormSumParams {
+    const float* part_h;
+    const float* part_y;
+    const void* w_post;
+    const void* gate;
+    float* dw_post;
+    float* dgate;
+    float* dw_pre;
+    int n, parts, groups, chunks;   // parts = groups * chunks rows of partial sums; whole: parts rows, groups = 1
+    float h_scale;
+    int whole;
+};
+
+// Column sums of the workgroups' partial sums: 64 columns a workgroup, 16 threads a column.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const NormSumParams p) {
+    __shared__ float red[16][64];
+    const int col = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    const bool in = col < p.n;
+    auto column = [&](const float* part, int first, int count) {
+        float s = 0.0f;
+        if (in)
+#pragma unroll 4
+            for (int i = slice; i < count; i += 16) s += part[(int64_t)(first + i) * p.n + col];
+        red[slice][threadIdx.x & 63] = s;
+        __syncthreads();
+        if (slice == 0)
+#pragma unroll
+            for (int i = 1; i < 16; ++i) s += red[i][threadIdx.x & 63];
+        __syncthreads();
+        return s;
+    };
+    if (p.dw_pre != nullptr) {
+        const float s = column(p.part_y, 0, p.parts);
+        if (slice == 0 && in) p.dw_pre[col] = s;
+    }
+    if (p.part_h == nullptr) return;
+    float wp = 1.0f, total = 0.0f;
+    if (in) {
+        float f[1];
+        load_or<T, 1>(p.w_post, col, f, 1.0f);
+        wp = f[0];
+    }
+    for (int g = 0; g < p.groups; ++g) {
+        const float s = column(p.part_h, g * p.chunks, p.chunks);
+        if (slice != 0 || !in) continue;
+        float f[1] = {1.0f};
+        if (!p.whole) {
+            load_or<T, 1>(p.gate != nullptr ? (const T*)p.gate + (int64_t)g * p.n : nullptr, col, f, 1.0f);
+            if (p.dgate != nullptr) p.dgate[(int64_t)g * p.n + col] = p.h_scale * wp * s;
+        }
+        total = __builtin_fmaf(f[0], s, total);
+    }
+    if (slice == 0 && in && p.dw_post != nullptr) p.dw_post[col] = p.h_scale * total;
+}
+
+// Threads of a workgroup and pieces a thread for a row of `pieces` pieces.
+struct RowShape { int nt, vpt; };
+RowShape row_shape(int pieces) {
+    if (pieces <= 64) return {64, 1};
+    if (pieces <= 128) return {128, 1};
+    if (pieces <= 256) return {256, 1};
+    if (pieces <= 512) return {512, 1};
+    if (pieces <= 1024) return {1024, 1};
+    if (pieces <= 4096) return {1024, 4};
+    return {1024, 32};
+}
+
+template <typename T, int W, bool OUT8>
+void launch_fwd(const NormParams& p, hipStream_t stream) {
+    const RowShape s = row_shape((p.n + W - 1) / W);
+    const dim3 grid((unsigned)p.rows);
+#define ROV_FWD(NT, VPT) hipLaunchKernelGGL((norm_fwd_kernel<T, W, NT, VPT, OUT8>), grid, dim3(NT), 0, stream, p)
+    if (s.nt == 64) ROV_FWD(64, 1);
+    else if (s.nt == 128) ROV_FWD(128, 1);
+    else if (s.nt == 256) ROV_FWD(256, 1);
+    else if (s.nt == 512) ROV_FWD(512, 1);
+    else if (s.vpt == 1) ROV_FWD(1024, 1);
+    else if (W > 4 || s.vpt == 4) ROV_FWD(1024, 4);
+    else if constexpr (W <= 4) ROV_FWD(1024, (W == 1 ? 32 : 8));
+#undef ROV_FWD
+}
+
+template <typename T, int W, bool WHOLE>
+void launch_bwd(const NormBwdParams& p, int blocks, hipStream_t stream) {
+    const RowShape s = row_shape((p.n + W - 1) / W);
+    const dim3 grid((unsigned)blocks);
+#define ROV_BWD(NT, VPT) hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, VPT, WHOLE>), grid, dim3(NT), 0, stream, p)
+    if (s.nt == 64) ROV_BWD(64, 1);
+    else if (s.nt == 128) ROV_BWD(128, 1);
+    else if (s.nt == 256) ROV_BWD(256, 1);
+    else if (s.nt == 512) ROV_BWD(512, 1);
+    else if (s.vpt == 1) ROV_BWD(1024, 1);
+    else if (W > 4 || s.vpt == 4) ROV_BWD(1024, 4);
+    else if constexpr (W <= 4) ROV_BWD(1024, (W == 1 ? 32 : 8));
+#undef ROV_BWD
+}
+
+// How the rows are shared: `blocks` workgroups, `chunks` of them a group of rows with one gate, or (whole) every
+// workgroup takes whole groups.
+struct RowSplit { int blocks, chunks; bool whole; };
+RowSplit split_rows(int64_t rows, int64_t rows_per_gate, int pieces) {
+    const int64_t groups = rows / rows_per_gate;
+    const int64_t most = (int64_t)device_cu_count() * (1024 / row_shape(pieces).nt);
+    int64_t want = rows / 4 < 1 ? 1 : rows / 4;
+    if (want > most) want = most;
+    if (groups > want) return {(int)want, 1, true};
+    int64_t chunks = want / groups;
+    if (chunks > rows_per_gate) chunks = rows_per_gate;
+    return {(int)(groups * chunks), (int)chunks, false};
+}
+int row_pieces(int n, int dtype) { return dtype == ROV_F32 ? (n % 4 == 0 ? n / 4 : n) : (n % 8 == 0 ? n / 8 : n); }
+
+int check_norm_sizes(int64_t rows, int n, int64_t rows_per_gate, int dtype, float x_scale, float h_scale, float eps) {
+    if (rows <= 0 || n <= 0 || rows_per_gate <= 0 || rows % rows_per_gate != 0) return ROV_ERR_INVALID;
+    if (!(eps > 0.0f) || !isfinite(eps) || !isfinite(x_scale) || !isfinite(h_scale)) return ROV_ERR_INVALID;
+    if (dtype != ROV_F32 && dtype != ROV_BF16) return dtype == ROV_FP8_E4M3 ? ROV_ERR_UNSUPPORTED : ROV_ERR_INVALID;
+    if (n > kMaxRow || rows > 0x7FFFFFFF) return ROV_ERR_UNSUPPORTED;
+    return ROV_OK;
+}
+
+}  // namespace
+
+int check_norm_residual(const void* x, const void* h, const void* w_post, const void* gate, const void* w_pre, const void* y,
+                        const void* yn, int64_t rows, int n, const int64_t ld[4], int64_t rows_per_gate, int dtype, float x_scale,
+                        float h_scale, float eps, float yn_fp8_scale) {
+    if (x == nullptr || h == nullptr || y == nullptr || ld == nullptr || (w_pre == nullptr) != (yn == nullptr)) return ROV_ERR_INVALID;
+    const int rc = check_norm_sizes(rows, n, rows_per_gate, dtype, x_scale, h_scale, eps);
+    if (rc != ROV_OK) return rc;
+    const size_t esz = dtype == ROV_F32 ? 4 : 2;
+    const bool out8 = yn_fp8_scale != 0.0f;
+    if (out8 && !(yn_fp8_scale > 0.0f && isfinite(yn_fp8_scale))) return ROV_ERR_INVALID;
+    if (out8 && dtype != ROV_BF16) return ROV_ERR_UNSUPPORTED;
+    const void* const all[] = {x, h, w_post, gate, w_pre, y, out8 ? nullptr : yn};
+    for (const void* q : all)
+        if (!aligned(q, esz)) return ROV_ERR_INVALID;
+    for (int i = 0; i < (w_pre != nullptr ? 4 : 3); ++i)
+        if (ld[i] < n && rows > 1) return ROV_ERR_INVALID;
+    return ROV_OK;
+}
+
+int launch_norm_residual(const void* x, const void* h, const void* w_post, const void* gate, const void* w_pre, void* y, void* yn,
+                         int64_t rows, int n, const int64_t ld[4], int64_t rows_per_gate, int dtype, float x_scale, float h_scale,
+                         float eps, float yn_fp8_scale, hipStream_t stream) {
+    {
+        const int rc = check_norm_residual(x, h, w_post, gate, w_pre, y, yn, rows, n, ld, rows_per_gate, dtype, x_scale, h_scale, eps,
+                                           yn_fp8_scale);
+        if (rc != ROV_OK) return rc;
+    }
+    const bool out8 = yn_fp8_scale != 0.0f;
+    NormParams p{x, h, w_post, gate, w_pre, y, yn, ld[0], ld[1], ld[2], ld[3], (int)rows, n, (int)rows_per_gate,
+                 x_scale, h_scale, eps, 1.0f / (float)n, out8 ? 1.0f / yn_fp8_scale : 1.0f};
+    const int w = dtype == ROV_F32 ? 4 : 8;
+    bool vec = n % w == 0;
+    const void* const all[] = {x, h, w_post, gate, w_pre, y, out8 ? nullptr : yn};
+    for (const void* q : all) vec = vec && aligned(q, 16);
+    for (int i = 0; i < 3; ++i) vec = vec && ld[i] % w == 0;
+    if (yn != nullptr) vec = vec && ld[3] % w == 0 && aligned(yn, 8);
+    if (dtype == ROV_F32) vec ? launch_fwd<float, 4, false>(p, stream) : launch_fwd<float, 1, false>(p, stream);
+    else if (out8) vec ? launch_fwd<uint16_t, 8, true>(p, stream) : launch_fwd<uint16_t, 1, true>(p, stream);
+    else vec ? launch_fwd<uint16_t, 8, false>(p, stream) : launch_fwd<uint16_t, 1, false>(p, stream);
+    ROV_LAUNCH_CHECK();
+    return ROV_OK;
+}
+
+}  // namespace rov
+
+extern "C" int rov_norm_residual(const void* x, const void* h, const void* w_post, const void* gate, const void* w_pre, void* y,
+                                 void* yn, int64_t rows, int n, const int64_t ld[4], int64_t rows_per_gate, int dtype, float x_scale,
+                                 float h_scale, float eps, float yn_fp8_scale, void* stream) {
+    return rov::launch_norm_residual(x, h, w_post, gate, w_pre, y, yn, rows, n, ld, rows_per_gate, dtype, x_scale, h_scale, eps,
+                                     yn_fp8_scale, (hipStream_t)stream);
+}
+
+extern "C" size_t rov_norm_residual_bwd_workspace_bytes(int64_t rows, int n, int64_t rows_per_gate, int dtype) {
+    if (rov::check_norm_sizes(rows, n, rows_per_gate, dtype, 1.0f, 1.0f, 1.0f) != ROV_OK) return 0;
+    // (the split of rows off 16 bytes, with a thread an element, has no more workgroups)
+    return 2 * sizeof(float) * (size_t)n * (size_t)rov::split_rows(rows, rows_per_gate, rov::row_pieces(n, dtype)).blocks;
+}
+
+extern "C" int rov_norm_residual_bwd(const void* y, const void* h, const void* w_post, const void* gate, const void* w_pre,
+                                     const void* dy, const void* dn, void* dx, void* dh, float* dw_post, float* dgate, float* dw_pre,
+                                     int64_t rows, int n, const int64_t ld[6], int64_t rows_per_gate, int dtype, float x_scale,
+                                     float h_scale, float eps, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace rov;
+    int rc = check_norm_sizes(rows, n, rows_per_gate, dtype, x_scale, h_scale, eps);
+    if (rc != ROV_OK && rc != ROV_ERR_UNSUPPORTED) return rc;
+    const bool pre = w_pre != nullptr, sums_h = dw_post != nullptr || dgate != nullptr;
+    if (ld == nullptr || (dx == nullptr && dh == nullptr && !sums_h && dw_pre == nullptr)) return ROV_ERR_INVALID;
+    if (pre != (dn != nullptr) || (pre && y == nullptr) || (!pre && dy == nullptr)) return ROV_ERR_INVALID;
+    if ((dw_pre != nullptr && !pre) || (dw_post != nullptr && w_post == nullptr) || (dgate != nullptr && gate == nullptr))
+        return ROV_ERR_INVALID;
+    if ((w_post != nullptr || dgate != nullptr) && h == nullptr) return ROV_ERR_INVALID;
+    const size_t esz = dtype == ROV_F32 ? 4 : 2;
+    const void* const vectors[] = {w_post, gate, w_pre};
+    const void* const tensors[6] = {pre ? y : nullptr, h, dy, dn, dx, dh};
+    for (const void* q : vectors)
+        if (!aligned(q, esz)) return ROV_ERR_INVALID;
+    for (int i = 0; i < 6; ++i) {
+        if (!aligned(tensors[i], esz)) return ROV_ERR_INVALID;
+        if (tensors[i] != nullptr && rows > 1 && ld[i] < n) return ROV_ERR_INVALID;
+    }
+    if (!aligned(dw_post, 4) || !aligned(dgate, 4) || !aligned(dw_pre, 4)) return ROV_ERR_INVALID;
+    if (rc != ROV_OK) return rc;
+    const int w = dtype == ROV_F32 ? 4 : 8;
+    bool vec = n % w == 0;
+    for (const void* q : vectors) vec = vec && aligned(q, 16);
+    for (int i = 0; i < 6; ++i)
+        if (tensors[i] != nullptr) vec = vec && aligned(tensors[i], 16) && ld[i] % w == 0;
+    const RowSplit sp = split_rows(rows, rows_per_gate, row_pieces(n, dtype));
+    const bool sums = sums_h || dw_pre != nullptr;
+    if (sums) {
+        if (workspace == nullptr || !aligned(workspace, 16)) return ROV_ERR_INVALID;
+        if (workspace_bytes < rov_norm_residual_bwd_workspace_bytes(rows, n, rows_per_gate, dtype)) return ROV_ERR_WORKSPACE;
+    }
+    float* const part = (float*)workspace;
+    NormBwdParams p{y, h, w_post, gate, w_pre, dy, dn, dx, dh, sp.whole ? dgate : nullptr,
+                    sums_h ? part : nullptr, dw_pre != nullptr ? part + (size_t)sp.blocks * n : nullptr,
+                    ld[0], ld[1], ld[2], ld[3], ld[4], ld[5], (int)rows, n, (int)rows_per_gate, sp.chunks,
+                    (int)(rows / rows_per_gate), x_scale, h_scale, eps, 1.0f / (float)n};
+    hipStream_t st = (hipStream_t)stream;
+    if (sp.whole) {
+        if (dtype == ROV_F32) vec ? launch_bwd<float, 4, true>(p, sp.blocks, st) : launch_bwd<float, 1, true>(p, sp.blocks, st);
+        else vec ? launch_bwd<uint16_t, 8, true>(p, sp.blocks, st) : launch_bwd<uint16_t, 1, true>(p, sp.blocks, st);
+    } else {
+        if (dtype == ROV_F32) vec ? launch_bwd<float, 4, false>(p, sp.blocks, st) : launch_bwd<float, 1, false>(p, sp.blocks, st);
+        else vec ? launch_bwd<uint16_t, 8, false>(p, sp.blocks, st) : launch_bwd<uint16_t, 1, false>(p, sp.blocks, st);
+    }
+    ROV_LAUNCH_CHECK();
+    if (!sums) return ROV_OK;
+    NormSumParams s{p.part_h, p.part_y, w_post, gate, dw_post, sp.whole ? nullptr : dgate, dw_pre, n, sp.blocks,
+                    sp.whole ? 1 : p.groups, sp.whole ? sp.blocks : sp.chunks, h_scale, sp.whole ? 1 : 0};
+    const dim3 grid((unsigned)((n + 63) / 64));
+    if (dtype == ROV_F32) hipLaunchKernelGGL((norm_sum_kernel<float>), grid, dim3(1024), 0, st, s);
+    else hipLaunchKernelGGL((norm_sum_kernel<uint16_t>), grid, dim3(1024), 0, st, s);
+    ROV_LAUNCH_CHECK();
+    return ROV_OK;
+}

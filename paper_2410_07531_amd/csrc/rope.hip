@@ -1,0 +1,227 @@
+// Rotary positions for queries and keys (the embedding inside the paper's Fig. 2 block in its Llama form), as
+// an operator of its own: adjacent or split pairs, the whole head or its first `rot` elements, the frequencies of
+// long-context scalings, any positions, any strides, forward and backward (the rotation by the negated angle).
+//
+// Pair p of a head, (a, b), at position s becomes m * (a cos t - b sin t, a sin t + b cos t), t = s * f_p.
+// What bounds it: memory, every element read and written once.  The sines of a token serve all its heads, so a
+// workgroup owns TPB tokens, forms their rot / 2 sines once into LDS and then walks over the heads, 16 bytes
+// a thread.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "rov_internal.h"
+#include "row_device.h"
+
+namespace rov {
+namespace {
+
+constexpr int kMaxHead = 512;
+
+struct RopeParams {
+    const void* src[2];          // Q, K
+    void* dst[2];
+    int64_t sb[2], ss[2], sh[2]; // strides of src: batch, token, head (elements)
+    int64_t db[2], ds[2], dh[2]; // of dst
+    const int64_t* positions;
+    int64_t positions_stride;
+    int64_t tokens;
+    int S, H, heads;             // heads = H + Hkv
+    int d, rot, copy;            // copy: elements behind `rot` go along (0 in place)
+    double log2_theta, inv_factor, low, inv_width, turns;   // turns: trained_len / (2 pi)
+    int scaling;
+    float magnitude, sign;
+};
+
+// Sine and cosine of position * frequency(p).  The angle is formed and reduced modulo 2 pi in double, so that
+// positions of a million keep fp32-accurate sines.
+__device__ __forceinline__ void rope_sincos(const RopeParams& p, int64_t pos, int pair, float* sn, float* cs) {
+    double f = exp2(-2.0 * (double)pair / (double)p.rot * p.log2_theta);
+    if (p.scaling == ROV_ROPE_SCALE_LINEAR) f *= p.inv_factor;
+    if (p.scaling == ROV_ROPE_SCALE_PARTS) {
+        double keep = (p.turns * f - p.low) * p.inv_width;
+        keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+        f *= keep + (1.0 - keep) * p.inv_factor;
+    }
+    double ang = (double)pos * f;
+    ang -= 6.283185307179586476925 * rint(ang * 0.15915494309189533577);
+    float s, c;
+    sincosf((float)ang, &s, &c);
+    *sn = s * p.magnitude * p.sign;
+    *cs = c * p.magnitude;
+}
+
+// W: elements a thread moves at once (16 bytes), or 1 where rows, heads or `rot` are off 16 bytes.
+// A unit of a head is W pairs (split layout: W elements of each half), max(1, W / 2) pairs (adjacent), or W elements to copy.
+template <typename T, int W, bool HALVES, int TPB>
+__global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
+    extern __shared__ __attribute__((aligned(16))) float lds[];   // [TPB][rot / 2] sines, then cosines
+    const int half = p.rot / 2;
+    float* const sines = lds;
+    float* const cosines = lds + TPB * half;
+    // beside a co-resident RNG grid the waves would wait for issue slots behind its long integer multiplies
+    __builtin_amdgcn_s_setprio(3);
+    const int64_t token0 = (int64_t)blockIdx.x * TPB;
+    for (int i = threadIdx.x; i < TPB * half; i += 256) {
+        const int tk = i / half;
+        const int64_t token = token0 + tk;
+        if (token >= p.tokens) break;
+        const int64_t b = token / p.S, s = token - b * p.S;
+        const int64_t pos = p.positions != nullptr ? p.positions[b * p.positions_stride + s] : s;
+        rope_sincos(p, pos, i - tk * half, &sines[i], &cosines[i]);
+    }
+    __syncthreads();
+    constexpr int P = HALVES ? W : (W > 1 ? W / 2 : 1);    // pairs of a unit
+    const int turn_units = half / P, units = turn_units + p.copy / W;
+    for (int tk = 0; tk < TPB; ++tk) {
+        const int64_t token = token0 + tk;
+        if (token >= p.tokens) return;
+        const int64_t b = token / p.S, s = token - b * p.S;
+        for (int i = threadIdx.x; i < p.heads * units; i += 256) {
+            const int head = i / units, u = i - head * units;
+            const int k = head >= p.H;
+            const int hh = k ? head - p.H : head;
+            const T* src = (const T*)p.src[k] + b * p.sb[k] + s * p.ss[k] + (int64_t)hh * p.sh[k];
+            T* dst = (T*)p.dst[k] + b * p.db[k] + s * p.ds[k] + (int64_t)hh * p.dh[k];
+            if (u >= turn_units) {
+                const int e = p.rot + (u - turn_units) * W;
+                Piece<T, W> v;
+                v.load(src + e);
+                v.store(dst + e);
+                continue;
+            }
+            const float* sn = sines + tk * half + u * P;
+            const float* cs = cosines + tk * half + u * P;
+            if constexpr (HALVES || W == 1) {
+                // split pairs; one element of each also serves adjacent pairs off 16 bytes
+                const int ea = HALVES ? u * W : 2 * u, eb = HALVES ? half + u * W : 2 * u + 1;
+                Piece<T, W> va, vb;
+                va.load(src + ea);
+                vb.load(src + eb);
+                float a[W], c[W];
+                va.get(a);
+                vb.get(c);
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    const float x = a[j], y = c[j];
+                    a[j] = x * cs[j] - y * sn[j];
+                    c[j] = x * sn[j] + y * cs[j];
+                }
+                va.set(a);
+                vb.set(c);
+                va.store(dst + ea);
+                vb.store(dst + eb);
+            } else {
+                Piece<T, W> v;
+                v.load(src + u * W);
+                float a[W];
+                v.get(a);
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const float x = a[2 * j], y = a[2 * j + 1];
+                    a[2 * j] = x * cs[j] - y * sn[j];
+                    a[2 * j + 1] = x * sn[j] + y * cs[j];
+                }
+                v.set(a);
+                v.store(dst + u * W);
+            }
+        }
+    }
+}
+
+template <typename T, int W, bool HALVES>
+int launch_form(const RopeParams& p, hipStream_t stream) {
+    // four tokens a workgroup while that still fills the chip eightfold
+    const int tpb = p.tokens >= (int64_t)device_cu_count() * 32 ? 4 : 1;
+    const int64_t blocks = (p.tokens + tpb - 1) / tpb;
+    if (blocks > 0x7FFFFFFF) return ROV_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((tpb == 4 ? rope_kernel<T, W, HALVES, 4> : rope_kernel<T, W, HALVES, 1>), dim3((unsigned)blocks), dim3(256),
+                       (size_t)tpb * p.rot * sizeof(float), stream, p);
+    ROV_LAUNCH_CHECK();
+    return ROV_OK;
+}
+
+}  // namespace
+
+int check_rope_cfg(const rov_rope_cfg* c, int d) {
+    if (c == nullptr || d <= 0) return ROV_ERR_INVALID;
+    if (c->layout != ROV_ROPE_INTERLEAVED && c->layout != ROV_ROPE_HALVES) return ROV_ERR_INVALID;
+    if (c->rot <= 0 || c->rot % 2 != 0 || c->rot > d || !(c->theta > 0.0f) || !isfinite(c->theta) || !isfinite(c->magnitude))
+        return ROV_ERR_INVALID;
+    if (c->scaling != ROV_ROPE_SCALE_NONE && c->scaling != ROV_ROPE_SCALE_LINEAR && c->scaling != ROV_ROPE_SCALE_PARTS)
+        return ROV_ERR_INVALID;
+    if (c->scaling != ROV_ROPE_SCALE_NONE && (!(c->factor > 0.0f) || !isfinite(c->factor))) return ROV_ERR_INVALID;
+    if (c->scaling == ROV_ROPE_SCALE_PARTS &&
+        (c->trained_len <= 0 || !(c->turns_low >= 0.0f) || !(c->turns_high > c->turns_low) || !isfinite(c->turns_high)))
+        return ROV_ERR_INVALID;
+    return d > kMaxHead ? ROV_ERR_UNSUPPORTED : ROV_OK;
+}
+
+int check_rope(const rov_rope_cfg* c, const void* Q, const void* Qo, const void* K, const void* Ko, int B, int S, int H, int Hkv,
+               int d, const int64_t strides[12], int dtype) {
+    const int rc = check_rope_cfg(c, d);
+    if (rc != ROV_OK && rc != ROV_ERR_UNSUPPORTED) return rc;
+    if (Q == nullptr || Qo == nullptr || strides == nullptr || B <= 0 || S <= 0 || H <= 0 || Hkv < 0) return ROV_ERR_INVALID;
+    if (Hkv > 0 && (K == nullptr || Ko == nullptr)) return ROV_ERR_INVALID;
+    if (dtype != ROV_F32 && dtype != ROV_BF16) return dtype == ROV_FP8_E4M3 ? ROV_ERR_UNSUPPORTED : ROV_ERR_INVALID;
+    const size_t esz = dtype == ROV_F32 ? 4 : 2;
+    if (!aligned(Q, esz) || !aligned(Qo, esz) || (Hkv > 0 && (!aligned(K, esz) || !aligned(Ko, esz)))) return ROV_ERR_INVALID;
+    // a buffer turned in place is its own result, stride for stride
+    for (int t = 0; t < (Hkv > 0 ? 2 : 1); ++t)
+        if ((t ? K : Q) == (t ? Ko : Qo))
+            for (int i = 0; i < 3; ++i)
+                if (strides[6 * t + i] != strides[6 * t + 3 + i]) return ROV_ERR_INVALID;
+    if ((int64_t)H + Hkv > 0x7FFFFFFF / kMaxHead) return ROV_ERR_UNSUPPORTED;
+    return rc;
+}
+
+int launch_rope_cfg(const rov_rope_cfg* c, const void* Q, void* Qo, const void* K, void* Ko, int B, int S, int H, int Hkv, int d,
+                    const int64_t strides[12], int dtype, const int64_t* positions, int64_t positions_stride, int backward,
+                    hipStream_t stream) {
+    {
+        const int rc = check_rope(c, Q, Qo, K, Ko, B, S, H, Hkv, d, strides, dtype);
+        if (rc != ROV_OK) return rc;
+    }
+    RopeParams p{};
+    p.src[0] = Q; p.src[1] = K; p.dst[0] = Qo; p.dst[1] = Ko;
+    const int64_t esz = dtype == ROV_F32 ? 4 : 2, w = 16 / esz;
+    bool vec = d % w == 0 && c->rot % (c->layout == ROV_ROPE_HALVES ? 2 * w : w) == 0;
+    bool copy = false;
+    for (int t = 0; t < 2; ++t) {
+        p.sb[t] = strides[6 * t]; p.ss[t] = strides[6 * t + 1]; p.sh[t] = strides[6 * t + 2];
+        p.db[t] = strides[6 * t + 3]; p.ds[t] = strides[6 * t + 4]; p.dh[t] = strides[6 * t + 5];
+        if (t == 1 && Hkv == 0) break;
+        vec = vec && aligned(p.src[t], 16) && aligned(p.dst[t], 16);
+        for (int i = 0; i < 6; ++i) vec = vec && strides[6 * t + i] % w == 0;
+        copy = copy || p.src[t] != p.dst[t];
+    }
+    p.positions = positions; p.positions_stride = positions_stride;
+    p.tokens = (int64_t)B * S;
+    p.S = S; p.H = H; p.heads = H + Hkv;
+    p.d = d; p.rot = c->rot; p.copy = copy ? d - c->rot : 0;
+    p.log2_theta = log2((double)c->theta);
+    p.scaling = c->scaling;
+    p.inv_factor = c->scaling == ROV_ROPE_SCALE_NONE ? 1.0 : 1.0 / (double)c->factor;
+    if (c->scaling == ROV_ROPE_SCALE_PARTS) {
+        p.low = c->turns_low;
+        p.inv_width = 1.0 / ((double)c->turns_high - (double)c->turns_low);
+        p.turns = (double)c->trained_len / 6.283185307179586476925;
+    }
+    p.magnitude = c->magnitude;
+    p.sign = backward ? -1.0f : 1.0f;
+    const bool halves = c->layout == ROV_ROPE_HALVES;
+    if (dtype == ROV_BF16)
+        return vec ? (halves ? launch_form<uint16_t, 8, true>(p, stream) : launch_form<uint16_t, 8, false>(p, stream))
+                   : (halves ? launch_form<uint16_t, 1, true>(p, stream) : launch_form<uint16_t, 1, false>(p, stream));
+    return vec ? (halves ? launch_form<float, 4, true>(p, stream) : launch_form<float, 4, false>(p, stream))
+               : (halves ? launch_form<float, 1, true>(p, stream) : launch_form<float, 1, false>(p, stream));
+}
+
+}  // namespace rov
+
+extern "C" int rov_rope(const rov_rope_cfg* cfg, const void* Q, void* Qo, const void* K, void* Ko, int B, int S, int H, int Hkv,
+                        int d, const int64_t strides[12], int dtype, const int64_t* positions, int64_t positions_stride,
+                        int backward, void* stream) {
+    return rov::launch_rope_cfg(cfg, Q, Qo, K, Ko, B, S, H, Hkv, d, strides, dtype, positions, positions_stride, backward,
+                                (hipStream_t)stream);
+}
