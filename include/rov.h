@@ -603,7 +603,7 @@ int rov_norm_residual_bwd(const void *y, const void *h, const void *w_post, cons
  *     lse[m] = log sum_v exp z[m][v],   loss[m] = lse[m] - z[m][targets[m]],
  * both fp32 [M], for every row: reductions are the caller's.  targets: int64 [M]; a row whose target is ignore_index (which must
  * lie outside [0, V)) has loss 0 and no gradient, whatever its X holds; any other target outside [0, V) gives a NaN loss (and NaN gradients).
- * dtype of X and W: ROV_F32 or ROV_BF16; row strides ldx, ldw >= K in elements.  Logits and sums are fp32.
+ * scale > 0.  dtype of X and W: ROV_F32 or ROV_BF16; row strides ldx, ldw >= K in elements.  Logits and sums are fp32.
  * vocab_piece: columns of a piece (rounded up to 256), 0: chosen by the library; it sets the workspace's size and
  * does not change what is computed beyond the order of fp32 sums.
  * workspace: 256-byte aligned device scratch of rov_linear_xent_workspace_bytes (0 for invalid arguments). */

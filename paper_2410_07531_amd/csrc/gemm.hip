@@ -212,13 +212,17 @@ __device__ __forceinline__ void epilogue_combine(int epi, uint2 r, float& c0, fl
 // is produced; C then points at bytes.
 // RAGGED: rows of any multiple of 16 bytes (k ends inside the last slot: its lanes beyond k are aimed outside the operands,
 // one select a load, and read zeros) and any number of output columns.
-template <int NJ, bool FP8, bool DUAL = false, bool OUT8 = false, bool RAGGED = false>
+// HEAD: the products of the loss over the vocabulary (HeadArgs; bf16, rows of any stride): the epilogue keeps the row statistics of
+// the tile's logits (HEAD_STATS), or the gradients of its logits (HEAD_GRAD), or adds the tile to fp32 sums (HEAD_SUM).
+template <int NJ, bool FP8, bool DUAL = false, bool OUT8 = false, bool RAGGED = false, int HEAD = 0>
 __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char* __restrict__ Wt,
                                           const char* __restrict__ Wt2, uint16_t* __restrict__ C,
                                           const uint16_t* __restrict__ R, int M, int N, int K, float alpha,
                                           int tiles_m, int tiles_n, int epi, char* lds, const int lane,
-                                          const int wave, float alpha2 = 1.0f, float out_inv = 1.0f) {
+                                          const int wave, float alpha2 = 1.0f, float out_inv = 1.0f,
+                                          const HeadArgs& head = HeadArgs{}) {
     static_assert(!OUT8 || DUAL, "e4m3 output exists in the dual form only");
+    static_assert(HEAD == 0 || (!FP8 && !DUAL && (HEAD != HEAD_GRAD || NJ == 8)), "the loss's products: plain bf16");
     static_assert(!RAGGED || (!FP8 && !DUAL), "rows off 128 bytes: the plain bf16 product only");
     constexpr bool MIXED = DUAL && NJ % 4 != 0;   // gate and up rows in every weight block
     const int wm = wave >> 1, wn = wave & 1;
@@ -278,7 +282,16 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     // Loads: wave w issues row blocks (8 rows) w, w+4, ... of each operand: 8 + NJ instructions
     // per slot.  Lane L fills physical chunk L%8 of row L/8, i.e. fetches logical chunk (L%8) ^ swz(row).
     const size_t ld_bytes = (size_t)K * ESZ;
-    const int ns = (int)((ld_bytes + (RAGGED ? kRow - 1 : 0)) / kRow);   // slots to walk
+    int ns = (int)((ld_bytes + (RAGGED ? kRow - 1 : 0)) / kRow);   // slots to walk
+    if constexpr (HEAD == HEAD_SUM) {   // this workgroup's share of k
+        const int s0 = (int)((int64_t)ns * blockIdx.y / gridDim.y), s1 = (int)((int64_t)ns * (blockIdx.y + 1) / gridDim.y);
+        ns = s1 - s0;
+        A += (size_t)s0 * kRow;
+        Wt += (size_t)s0 * kRow;
+    }
+    const size_t ld_a = HEAD ? head.ld_a : ld_bytes, ld_w = HEAD ? head.ld_w : ld_bytes;
+    // bytes of k that a row holds from the base on (the last row's end bounds the operand)
+    const size_t k_bytes = HEAD == HEAD_SUM ? (size_t)ns * kRow : ld_bytes;
     const int rows_a = M - m0 < BM ? M - m0 : BM;
     const int rows_w = N - n0 < BNT ? N - n0 : BNT;
     uint32_t voff_a[8], voff_w[NJ];
@@ -286,17 +299,21 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     for (int j = 0; j < 8; ++j) {
         const int row = (wave + 4 * j) * 8 + (lane >> 3);
         const int chunk = (lane & 7) ^ swz(row);
-        const int ra = row < rows_a ? row : rows_a - 1;   // rows past the edge are never stored
+        // HEAD_GRAD: LDS row 128*h + 16*i + r holds activation row 128*h + 8*r + i and weight row 128*h + 16*j + 4*g + e weight row
+        // 128*h + 32*g + 4*j + e, so that a lane ends up with eight consecutive rows and 32 consecutive columns of the tile
+        const int arow = HEAD == HEAD_GRAD ? (row & 128) | ((row & 15) << 3) | ((row >> 4) & 7) : row;
+        const int ra = arow < rows_a ? arow : rows_a - 1;   // rows past the edge are never stored
         // dual: LDS rows [16*NJ*h, +8*NJ) are gate rows of output columns 8*NJ*h .., the next 8*NJ the up rows;
         // mixed: LDS rows [16*b, +8) are gate rows of output columns 8*b .., the next 8 the up rows
         const int wcol = MIXED ? (row >> 4) * 8 + (row & 7)
                                : DUAL ? (row / (16 * NJ)) * (8 * NJ) + row % (8 * NJ) : row;
-        const int rw = wcol < rows_w ? wcol : rows_w - 1;
-        voff_a[j] = (uint32_t)((size_t)ra * ld_bytes) + (uint32_t)(chunk * 16);
-        if (j < NJ) voff_w[j] = (uint32_t)((size_t)rw * ld_bytes) + (uint32_t)(chunk * 16);
+        const int wrow = HEAD == HEAD_GRAD ? (row & 128) | (((row >> 2) & 3) << 5) | (((row >> 4) & 7) << 2) | (row & 3) : wcol;
+        const int rw = wrow < rows_w ? wrow : rows_w - 1;
+        voff_a[j] = (uint32_t)((size_t)ra * ld_a) + (uint32_t)(chunk * 16);
+        if (j < NJ) voff_w[j] = (uint32_t)((size_t)rw * ld_w) + (uint32_t)(chunk * 16);
     }
-    const char* a_panel = A + (size_t)m0 * ld_bytes;
-    const char* w_panel = Wt + (size_t)n0 * ld_bytes;
+    const char* a_panel = A + (size_t)m0 * ld_a;
+    const char* w_panel = Wt + (size_t)n0 * ld_w;
     // slot at which this workgroup starts its cyclic walk over k (the sum does not depend on the
     // order; the fp32 rounding does, deterministically)
     const int kstart = (int)((unsigned)tm % (unsigned)ns);
@@ -311,9 +328,10 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         r[3] = 0x00020000;
         return r;
     };
-    const i32x4 rsrc_a = make_rsrc(a_panel, (size_t)rows_a * ld_bytes);
+    const i32x4 rsrc_a = make_rsrc(a_panel, HEAD ? (size_t)(rows_a - 1) * ld_a + k_bytes : (size_t)rows_a * ld_bytes);
     // (mixed: a load fills 8 rows, row block wave + 4*j, so odd waves load the up rows)
-    const i32x4 rsrc_w = make_rsrc(MIXED && (wave & 1) ? Wt2 + (size_t)n0 * ld_bytes : w_panel, (size_t)rows_w * ld_bytes);
+    const i32x4 rsrc_w = make_rsrc(MIXED && (wave & 1) ? Wt2 + (size_t)n0 * ld_bytes : w_panel,
+                                   HEAD ? (size_t)(rows_w - 1) * ld_w + k_bytes : (size_t)rows_w * ld_bytes);
     const i32x4 rsrc_w2 = DUAL && !MIXED ? make_rsrc(Wt2 + (size_t)n0 * ld_bytes, (size_t)rows_w * ld_bytes) : rsrc_w;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lptr_t)lds;
     // RAGGED: does the lane's chunk (the same in every load: row / 2 % 8 does not depend on j) lie beyond k in the last slot?
@@ -489,6 +507,136 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     // D'[r][c] = C[m = c][n = r]: lane holds activation row lane%16 and weight rows 4*(lane/16) + e
     const int mrow = lane & 15;
     const int nsub = (lane >> 4) * 4;
+    if constexpr (HEAD == HEAD_STATS) {
+        // per row: maximum and sum of exp2 over this wave's 16*NJ columns (logits in units of log 2: alpha carries log2 e), and the
+        // target's logit where it is one of them
+        const int nw = n0 + wn * 16 * NJ;
+        const bool edge = nw + 16 * NJ > N;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            const int m = m0 + wm * 128 + i * 16 + mrow;
+            float v[NJ][4], top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[j][e] = acc_read(acc[j][i][e]);
+                    if (edge && nw + j * 16 + nsub + e >= N) v[j][e] = -INFINITY;
+                    top = fmaxf(top, v[j][e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            top *= alpha;
+            const float base = top > -INFINITY ? top : 0.0f;   // (no column, or all minus infinity: the sum is 0, not NaN)
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][e], alpha, -base));
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (lane < 16 && m < M) head.part[(size_t)(2 * tn + wn) * M + m] = make_float2(top, sum);
+            // the target's column within this wave, where it is one (few rows of few tiles)
+            const int64_t t = m < M ? head.targets[m] - head.v0 - nw : -1;
+            const bool mine = t >= 0 && t < 16 * NJ && t < N - nw && (((int)t >> 2) & 3) == (lane >> 4);
+            if (__ballot(mine) != 0) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (mine && (int)t == j * 16 + nsub + e) head.picked[m] = v[j][e] * alpha;
+            }
+        }
+        return;
+    }
+    if constexpr (HEAD == HEAD_GRAD) {
+        // gradients of the logits, G[m][n] and its transpose; rows that are ignored or beyond M and columns beyond N are zero, so that
+        // both can be walked in whole slots as the next products' k
+        const int mw = m0 + wm * 128 + 8 * mrow;          // first of this lane's eight rows
+        const int nl = n0 + wn * 128 + 8 * nsub;          // first of its 32 columns
+        float lse2[8], up[8], down[8];
+        int tcol[8];
+        bool keep[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int m = mw + i;
+            const int64_t t = m < M ? head.targets[m] : head.ignore;
+            keep[i] = t != head.ignore;
+            const float a = keep[i] ? (t >= 0 && t < head.vocab ? head.dloss[m] : NAN) : 0.0f;
+            const float b = keep[i] && head.dlse != nullptr ? head.dlse[m] : 0.0f;
+            lse2[i] = keep[i] ? head.lse[m] * 1.44269504088896341f : 0.0f;
+            up[i] = (a + b) * head.scale;
+            down[i] = a * head.scale;
+            const int64_t c = t - head.v0 - nl;
+            tcol[i] = keep[i] && c >= 0 && c < 32 ? (int)c : -1;
+        }
+#pragma unroll
+        for (int jj = 0; jj < NJ; jj += 2) {
+            __builtin_amdgcn_sched_barrier(0);
+            float g[8][8];   // [row][column 4*jj + c]
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc_read(acc[jj + (c >> 2)][i][c & 3]), alpha, -lse2[i]));
+                    float q = p * up[i];
+                    if (tcol[i] == 4 * jj + c) q -= down[i];
+                    g[i][c] = keep[i] && nl + 4 * jj + c < N ? q : 0.0f;
+                }
+            const int n = nl + 4 * jj;
+            if (head.g != nullptr && n < head.ld_g)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (mw + i < M)
+                        *reinterpret_cast<uint4*>(head.g + (size_t)(mw + i) * head.ld_g + n) =
+                            make_uint4(pack_bf16x2(g[i][0], g[i][1]), pack_bf16x2(g[i][2], g[i][3]), pack_bf16x2(g[i][4], g[i][5]),
+                                       pack_bf16x2(g[i][6], g[i][7]));
+            if (head.gt != nullptr && mw < head.ld_gt)
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (n + c < N)
+                        *reinterpret_cast<uint4*>(head.gt + (size_t)(n + c) * head.ld_gt + mw) =
+                            make_uint4(pack_bf16x2(g[0][c], g[1][c]), pack_bf16x2(g[2][c], g[3][c]), pack_bf16x2(g[4][c], g[5][c]),
+                                       pack_bf16x2(g[6][c], g[7][c]));
+        }
+        return;
+    }
+    if constexpr (HEAD == HEAD_SUM) {
+        // fp32 sums of the shares of k, rows of ld_sum values; or the result itself, bf16
+        float* const sums = head.sum != nullptr ? head.sum + (size_t)blockIdx.y * M * head.ld_sum : nullptr;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            const int m = m0 + wm * 128 + i * 16 + mrow;
+            if (m >= M) continue;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int n = n0 + wn * 16 * NJ + j * 16 + nsub;
+                if (n >= N) continue;
+                f32x4 c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c[e] = acc_read(acc[j][i][e]);
+                if (sums != nullptr) {
+                    f32x4* const at = reinterpret_cast<f32x4*>(sums + (size_t)m * head.ld_sum + n);   // (rows are padded to four columns)
+                    if (head.add) c += *at;
+                    *at = c;
+                } else {
+                    uint16_t* const out = C + (size_t)m * head.ld_out + n;
+                    const uint2 v = make_uint2(pack_bf16x2(c[0], c[1]), pack_bf16x2(c[2], c[3]));
+                    if (head.out_wide && n + 3 < N) {
+                        *reinterpret_cast<uint2*>(out) = v;
+                    } else {
+                        const uint32_t h[4] = {v.x & 0xFFFFu, v.x >> 16, v.y & 0xFFFFu, v.y >> 16};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (n + e < N) out[e] = (uint16_t)h[e];
+                    }
+                }
+            }
+        }
+        return;
+    }
     if constexpr (DUAL) {
         auto store4 = [&](int m, int n, const float (&o)[4]) {
             if (m >= M || n >= N) return;
@@ -601,6 +749,16 @@ __global__ __launch_bounds__(256, 1) void gemm_tn_kernel(const char* __restrict_
     __builtin_amdgcn_s_setprio(3);
     gemm_tile<NJ, FP8, false, false, RAGGED>(A, Wt, nullptr, C, R, M, N, K, alpha, tiles_m, tiles_n, epi, lds, threadIdx.x & 63,
                        __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+}
+
+// The products of the loss over the vocabulary (see gemm_tile, HEAD); HEAD_SUM: gridDim.y shares of k.
+template <int NJ, bool RAGGED, int HEAD>
+__global__ __launch_bounds__(256, 1) void gemm_head_kernel(const char* __restrict__ A, const char* __restrict__ Wt, uint16_t* __restrict__ C,
+                                                          int M, int N, int K, float alpha, int tiles_m, int tiles_n, const HeadArgs head) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    __builtin_amdgcn_s_setprio(3);
+    gemm_tile<NJ, false, false, false, RAGGED, HEAD>(A, Wt, nullptr, C, nullptr, M, N, K, alpha, tiles_m, tiles_n, EPI_ADD, lds,
+                                                     threadIdx.x & 63, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 1.0f, 1.0f, head);
 }
 
 // C[M, N] = silu(A Wg^T) * (A Wu^T): the SwiGLU of the block's feed-forward as one product with
@@ -860,6 +1018,34 @@ int best_tile_cols(int M, int N, int fixed = 1) {
         if (best < 0 || cost < best) { best = cost; nj = c; }
     }
     return 32 * nj;
+}
+
+int gemm_head_tiles_n(int N) { return (N + BN - 1) / BN; }
+
+int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
+                     hipStream_t stream) {
+    const bool ragged = K % 64 != 0;
+    if (A == nullptr || W == nullptr || M <= 0 || N <= 0 || K <= 0 || shares <= 0 || shares > 65535) return ROV_ERR_INVALID;
+    if (!aligned(A, 16) || !aligned(W, 16) || head.ld_a % 16 != 0 || head.ld_w % 16 != 0 || K % 8 != 0) return ROV_ERR_INVALID;
+    if (head.ld_a < (size_t)K * 2 || head.ld_w < (size_t)K * 2 || (kind == HEAD_SUM && (ragged || shares > K / 64))) return ROV_ERR_INVALID;
+    // a 256-row operand panel is addressed with 32-bit byte offsets
+    if ((unsigned long long)BM * head.ld_a + 1024 > 0xFFFFFFFFull || (unsigned long long)BN * head.ld_w + 1024 > 0xFFFFFFFFull)
+        return ROV_ERR_UNSUPPORTED;
+    typedef void (*kern_t)(const char*, const char*, uint16_t*, int, int, int, float, int, int, const HeadArgs);
+    static const kern_t sum[5] = {gemm_head_kernel<4, false, HEAD_SUM>, gemm_head_kernel<5, false, HEAD_SUM>, gemm_head_kernel<6, false, HEAD_SUM>,
+                                  gemm_head_kernel<7, false, HEAD_SUM>, gemm_head_kernel<8, false, HEAD_SUM>};
+    const int nj = kind == HEAD_SUM && shares == 1 ? best_tile_cols(M, N) / 32 : 8;
+    const kern_t kern = kind == HEAD_STATS  ? (ragged ? gemm_head_kernel<8, true, HEAD_STATS> : gemm_head_kernel<8, false, HEAD_STATS>)
+                        : kind == HEAD_GRAD ? (ragged ? gemm_head_kernel<8, true, HEAD_GRAD> : gemm_head_kernel<8, false, HEAD_GRAD>)
+                                            : sum[nj - 4];
+    const int rc = set_max_dynamic_lds((const void*)kern, kLdsBytes);
+    if (rc != ROV_OK) return rc;
+    const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + 32 * nj - 1) / (32 * nj);
+    if (tiles_m * tiles_n > 0x7FFFFFFFLL) return ROV_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
+                       (uint16_t*)C, M, N, K, alpha, (int)tiles_m, (int)tiles_n, head);
+    ROV_LAUNCH_CHECK();
+    return ROV_OK;
 }
 
 // Is a sum of at most 128 terms done sooner by the any-shape kernel?  Its 64 x 64 tiles pay per 16 terms; the

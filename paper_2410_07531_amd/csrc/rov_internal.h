@@ -107,6 +107,37 @@ int launch_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, void* 
                            float scaleA, float scaleWg, float scaleWu, float scaleC, hipStream_t stream);
 int check_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, const void* C, int M, int N, int K,
                           float scaleC);
+// The products of the loss over the vocabulary (bf16, fp32 accumulation; A [M,K], W [N,K], K contiguous, K % 8 == 0, strides
+// ld_a, ld_w in bytes, multiples of 16), as forms of the 256-row kernel with other epilogues:
+//   HEAD_STATS  z = A W^T * alpha (logits in units of log 2): per row and half tile (128 columns) maximum and sum of exp2 to
+//               part[2 * gemm_head_tiles_n(N)][M], the target's z to picked[m] (rows whose target is one of the N columns);
+//   HEAD_GRAD   G[m][n] = scale * (exp2(z - lse log2 e) * (dloss + dlse) - [v0 + n == target] * dloss) in bf16 to g [M][ld_g] and
+//               its transpose to gt [N][ld_gt] (either may be NULL); columns N .. ld_g and rows M .. ld_gt are zero (ld_g, ld_gt: K of the next products,
+//               below the next multiple of 256), rows of ignored targets too;
+//   HEAD_SUM    C or fp32 sums of A W^T, K % 64 == 0: `shares` workgroups a tile take a share of k each and write (add: add to)
+//               sum[share][M][ld_sum]; sum == NULL (one share): bf16 to C, rows of ld_out (out_wide: rows on 8 bytes).
+enum { HEAD_STATS = 1, HEAD_GRAD = 2, HEAD_SUM = 3 };
+struct HeadArgs {
+    size_t ld_a = 0, ld_w = 0;
+    const int64_t* targets = nullptr;
+    float2* part = nullptr;
+    float* picked = nullptr;
+    const float* lse = nullptr;
+    const float* dloss = nullptr;
+    const float* dlse = nullptr;
+    uint16_t* g = nullptr;
+    uint16_t* gt = nullptr;
+    int64_t ld_g = 0, ld_gt = 0;
+    int64_t ignore = 0, v0 = 0, vocab = 0;
+    float scale = 1.0f;
+    float* sum = nullptr;
+    int64_t ld_sum = 0, ld_out = 0;
+    bool add = false, out_wide = false;
+};
+int gemm_head_tiles_n(int N);
+int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
+                     hipStream_t stream);
+
 // One kernel whose workgroups compute a tile of the bf16 GEMM with four waves while four more
 // waves generate keep-mask chunks pulled from queue slot `qslot` (paper Sec. 6.1: the single-kernel,
 // wave-specialised form of the overlap).  S % 32 == 0; what the RNG waves do not get to stays in
