@@ -49,7 +49,7 @@ __device__ __forceinline__ void load_or(const void* base, int at, float (&f)[W],
 // One workgroup of NT threads a row, VPT pieces of W elements a thread.  OUT8: yn is e4m3 bytes.
 template <typename T, int W, int NT, int VPT, bool OUT8>
 __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormParams p) {
-    __shared__ float red[2][NT / 64];
+    __shared__ float red[2][16];
     __builtin_amdgcn_s_setprio(3);   // beside a co-resident RNG grid: ahead of its long integer multiplies
     const int64_t row = blockIdx.x;
     const T* const x = (const T*)p.x + row * p.ld_x;
@@ -153,9 +153,11 @@ struct NormBwdParams {
 // whole groups (blockIdx.x, blockIdx.x + gridDim.x, ...), and keeps the column sums of its rows in registers.
 // Row sums: the sum behind dh's mean is linear in g, so its three parts are summed beside mean(y^2), mean(y t) and
 // mean(h^2) and one barrier a row is enough (two sets of scratch by the parity of the row).
+// With one piece a thread the next row is on its way while a row is worked on, and the weights stay in registers.
 template <typename T, int W, int NT, int VPT, bool WHOLE>
-__global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormBwdParams p) {
-    __shared__ float red[2][6][NT / 64];
+__global__ __launch_bounds__(NT, VPT == 1 ? 4 : 1) void norm_bwd_kernel(const NormBwdParams p) {
+    constexpr bool AHEAD = VPT == 1;
+    __shared__ float red[2][6 * 16];
     __builtin_amdgcn_s_setprio(3);
     float col_h[VPT][W], col_y[VPT][W], col_g[WHOLE ? VPT : 1][W];
 #pragma unroll
@@ -168,6 +170,40 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormBwdParams p) {
         }
     const bool has_pre = p.w_pre != nullptr, has_post = p.w_post != nullptr;
     const bool with_h = p.h != nullptr;
+    struct Row { Piece<T, W> y[VPT], h[VPT], dy[VPT], dn[VPT]; };
+    auto fetch = [&](Row& r, int64_t row) {
+#pragma unroll
+        for (int c = 0; c < VPT; ++c) {
+            const int e = (c * NT + (int)threadIdx.x) * W;
+            r.y[c].zero(); r.h[c].zero(); r.dy[c].zero(); r.dn[c].zero();
+            if (e < p.n) {
+                if (has_pre) {
+                    r.y[c].load((const T*)p.y + row * p.ld_y + e);
+                    r.dn[c].load((const T*)p.dn + row * p.ld_dn + e);
+                }
+                if (with_h) r.h[c].load((const T*)p.h + row * p.ld_h + e);
+                if (p.dy != nullptr) r.dy[c].load((const T*)p.dy + row * p.ld_dy + e);
+            }
+        }
+    };
+    Piece<T, W> ones, kept_pre, kept_post, kept_gate;
+    {
+        float f[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) f[j] = 1.0f;
+        ones.set(f);
+    }
+    kept_pre = kept_post = kept_gate = ones;
+    // a weight or gate of this thread's columns (ones without it): kept in registers where the row is one piece
+    auto vec = [&](const Piece<T, W>& kept, const void* base, int e) {
+        Piece<T, W> v = AHEAD ? kept : ones;
+        if (!AHEAD && base != nullptr) v.load((const T*)base + e);
+        return v;
+    };
+    if (AHEAD && (int)threadIdx.x * W < p.n) {
+        if (has_pre) kept_pre.load((const T*)p.w_pre + threadIdx.x * W);
+        if (has_post) kept_post.load((const T*)p.w_post + threadIdx.x * W);
+    }
     int parity = 0;
     for (int group = WHOLE ? (int)blockIdx.x : (int)blockIdx.x / p.chunks; group < p.groups; group += WHOLE ? (int)gridDim.x : p.groups) {
         int64_t r0 = (int64_t)group * p.rows_per_gate, r1 = r0 + p.rows_per_gate;
@@ -177,89 +213,63 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormBwdParams p) {
             r0 += len * chunk / p.chunks;
         }
         const T* const gate = p.gate != nullptr ? (const T*)p.gate + (int64_t)group * p.n : nullptr;
+        if (AHEAD && gate != nullptr && (int)threadIdx.x * W < p.n) kept_gate.load(gate + threadIdx.x * W);
+        Row cur, next;
+        if (AHEAD && r0 < r1) fetch(next, r0);
         for (int64_t row = r0; row < r1; ++row) {
-            Piece<T, W> yv[VPT], hv[VPT], dyv[VPT], dnv[VPT];
-#pragma unroll
-            for (int c = 0; c < VPT; ++c) {
-                const int e = (c * NT + (int)threadIdx.x) * W;
-                yv[c].zero(); hv[c].zero(); dyv[c].zero(); dnv[c].zero();
-                if (e < p.n) {
-                    if (has_pre) {
-                        yv[c].load((const T*)p.y + row * p.ld_y + e);
-                        dnv[c].load((const T*)p.dn + row * p.ld_dn + e);
-                    }
-                    if (with_h) hv[c].load((const T*)p.h + row * p.ld_h + e);
-                    if (p.dy != nullptr) dyv[c].load((const T*)p.dy + row * p.ld_dy + e);
-                }
+            if constexpr (AHEAD) {
+                cur = next;
+                if (row + 1 < r1) fetch(next, row + 1);
+            } else {
+                fetch(cur, row);
             }
             float sum[6] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int c = 0; c < VPT; ++c) {
                 const int e = (c * NT + (int)threadIdx.x) * W;
                 if (e >= p.n) continue;
-                float y[W], h[W], dy[W], t[W], wp[W], g[W], w[W];
-                yv[c].get(y); hv[c].get(h); dyv[c].get(dy); dnv[c].get(t);
-                load_or<T, W>(p.w_pre, e, w, 0.0f);
-                load_or<T, W>(p.w_post, e, wp, 0.0f);
-                load_or<T, W>(gate, e, g, 1.0f);
+                const Piece<T, W> w = vec(kept_pre, p.w_pre, e), wp = vec(kept_post, p.w_post, e), g = vec(kept_gate, gate, e);
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    t[j] *= w[j];
-                    const float u = h[j] * wp[j] * g[j];
-                    sum[0] = __builtin_fmaf(y[j], y[j], sum[0]);
-                    sum[1] = __builtin_fmaf(y[j], t[j], sum[1]);
-                    sum[2] = __builtin_fmaf(h[j], h[j], sum[2]);
-                    sum[3] = __builtin_fmaf(u, dy[j], sum[3]);
-                    sum[4] = __builtin_fmaf(u, t[j], sum[4]);
-                    sum[5] = __builtin_fmaf(u, y[j], sum[5]);
+                    const float y = cur.y[c].at(j), h = cur.h[c].at(j), t = cur.dn[c].at(j) * w.at(j), u = h * wp.at(j) * g.at(j);
+                    sum[0] = __builtin_fmaf(y, y, sum[0]);
+                    sum[1] = __builtin_fmaf(y, t, sum[1]);
+                    sum[2] = __builtin_fmaf(h, h, sum[2]);
+                    sum[3] = __builtin_fmaf(u, cur.dy[c].at(j), sum[3]);
+                    sum[4] = __builtin_fmaf(u, t, sum[4]);
+                    sum[5] = __builtin_fmaf(u, y, sum[5]);
+                    __builtin_amdgcn_sched_barrier(0);   // one element at a time: unpacked ahead they would spill
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 6; ++i) {
-#pragma unroll
-                for (int s = 32; s > 0; s >>= 1) sum[i] += __shfl_xor(sum[i], s);
-            }
-            if constexpr (NT > 64) {
-                if ((threadIdx.x & 63) == 0)
-#pragma unroll
-                    for (int i = 0; i < 6; ++i) red[parity][i][threadIdx.x >> 6] = sum[i];
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 6; ++i) {
-                    sum[i] = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < NT / 64; ++w) sum[i] += red[parity][i][w];
-                }
-                parity ^= 1;
-            }
+            workgroup_sums<NT, 6>(sum, red[parity]);
+            parity ^= 1;
             const float r = has_pre ? 1.0f / sqrtf(sum[0] * p.inv_n + p.eps) : 0.0f;
             const float rh = has_post ? 1.0f / sqrtf(sum[2] * p.inv_n + p.eps) : 1.0f;
-            const float my = r * r * r * sum[1] * p.inv_n;                      // y times this is hat * r * mean(hat t)
+            const float my = has_pre ? r * r * r * sum[1] * p.inv_n : 0.0f;     // y times this is hat * r * mean(hat t)
             const float mh = has_post ? rh * rh * rh * p.inv_n * p.h_scale * (sum[3] + r * sum[4] - my * sum[5]) : 0.0f;
 #pragma unroll
             for (int c = 0; c < VPT; ++c) {
                 const int e = (c * NT + (int)threadIdx.x) * W;
                 if (e >= p.n) continue;
-                float y[W], h[W], dy[W], dn[W], wp[W], g[W], w[W];
-                yv[c].get(y); hv[c].get(h); dyv[c].get(dy); dnv[c].get(dn);
-                load_or<T, W>(p.w_pre, e, w, 0.0f);
-                load_or<T, W>(p.w_post, e, wp, 1.0f);
-                load_or<T, W>(gate, e, g, 1.0f);
+                const Piece<T, W> w = vec(kept_pre, p.w_pre, e), wp = vec(kept_post, p.w_post, e), g = vec(kept_gate, gate, e);
+                float dx[W], dh[W];
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    const float gy = dy[j] + r * w[j] * dn[j] - y[j] * my;
-                    col_y[c][j] = __builtin_fmaf(dn[j] * r, y[j], col_y[c][j]);
-                    col_h[c][j] = __builtin_fmaf(gy * rh, h[j], col_h[c][j]);
-                    dy[j] = p.x_scale * gy;
-                    h[j] = rh * wp[j] * (p.h_scale * g[j] * gy) - h[j] * mh;
+                    const float y = cur.y[c].at(j), h = cur.h[c].at(j), dn = cur.dn[c].at(j);
+                    const float gy = cur.dy[c].at(j) + r * w.at(j) * dn - y * my;
+                    col_y[c][j] = __builtin_fmaf(dn * r, y, col_y[c][j]);
+                    col_h[c][j] = __builtin_fmaf(gy * rh, h, col_h[c][j]);
+                    dx[j] = p.x_scale * gy;
+                    dh[j] = rh * wp.at(j) * (p.h_scale * g.at(j) * gy) - h * mh;
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 Piece<T, W> out;
                 if (p.dx != nullptr) {
-                    out.set(dy);
+                    out.set(dx);
                     out.store((T*)p.dx + row * p.ld_dx + e);
                 }
                 if (p.dh != nullptr) {
-                    out.set(h);
+                    out.set(dh);
                     out.store((T*)p.dh + row * p.ld_dh + e);
                 }
             }

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void xent_stats_kernel(const float* __restrict
                                                          const int64_t* __restrict__ targets, int64_t ignore,
                                                          RowState* __restrict__ state, float* __restrict__ loss,
                                                          float* __restrict__ lse) {
-    __shared__ float red[8];
+    __shared__ float red[4 + 16];
     const int64_t row = blockIdx.x;
     const float* const zr = z + row * cols;
     float top = -INFINITY;
