@@ -6,6 +6,7 @@ fallback: if the library is missing or a call fails, an exception is raised.
 """
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "librov.so")
@@ -121,10 +122,10 @@ SIGNATURES = {
     "rov_block_static_scratch_bytes": (ctypes.c_size_t, []),
     "rov_block_forward_static": (_i, [ctypes.POINTER(BlockWeights), _p, _p, _i, _i, ctypes.POINTER(BlockCfg),
                                       _i, _u64, _u64, _i, _p, _p, _p, _p]),
-    "rov_rope": (_i, [ctypes.POINTER(RopeCfg), _p, _p, _p, _p, _i, _i, _i, _i, _i, ctypes.POINTER(_i64), _i, _p, _i64, _i, _p]),
-    "rov_norm_residual": (_i, [_p] * 7 + [_i64, _i, ctypes.POINTER(_i64), _i64, _i, _f, _f, _f, _f, _p]),
+    "rov_rope": (_i, [ctypes.POINTER(RopeCfg), _p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _i, _p, _i64, _i, _p]),
+    "rov_norm_residual": (_i, [_p] * 7 + [_i64, _i, _p, _i64, _i, _f, _f, _f, _f, _p]),
     "rov_norm_residual_bwd_workspace_bytes": (ctypes.c_size_t, [_i64, _i, _i64, _i]),
-    "rov_norm_residual_bwd": (_i, [_p] * 12 + [_i64, _i, ctypes.POINTER(_i64), _i64, _i, _f, _f, _f, _p, ctypes.c_size_t, _p]),
+    "rov_norm_residual_bwd": (_i, [_p] * 12 + [_i64, _i, _p, _i64, _i, _f, _f, _f, _p, ctypes.c_size_t, _p]),
     "rov_linear_xent_workspace_bytes": (ctypes.c_size_t, [_i] * 6),
     "rov_linear_xent": (_i, [_p, _p, _p, _i, _i, _i, _i64, _i64, _i, _f, _i64, _p, _p, _i, _p, ctypes.c_size_t, _p]),
     "rov_linear_xent_bwd": (_i, [_p] * 6 + [_i, _i, _i, _i64, _i64, _i, _f, _i64, _p, _p, _i64, _i64, _i, _p, ctypes.c_size_t, _p]),
@@ -560,92 +561,118 @@ def block_forward_static(weights, x, y, cfg, schedule, seed, offset, mask, main_
 
 # ---- operators around the block.  Results and workspaces that the caller does not bring come from torch's allocator, on
 # the stream that the call runs on (a block of another stream's pool could still be in use there).
-def _new(shape, dtype, device, stream):
+# Their small calls, too, are bound by this file (norms of 16 tokens: 16.3 us at first, 10.5 now; the kernel takes 4): what a call asks
+# of its tensors is asked once, in one pass, and names and messages are made only where something is refused.
+# strides go to ctypes packed (bytes are taken as a pointer to them): a quarter of the time of a ctypes array
+_pack4, _pack6, _pack12 = (struct.Struct("%dq" % n).pack for n in (4, 6, 12))
+_torch = _current_device = None
+
+
+def _start():
+    global _torch, _current_device
     import torch
+    torch.cuda.current_device()     # initialises the device
+    _torch, _current_device = torch, getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _new(shape, like, stream, dtype):
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+    with _torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _same(what, tensors):
-    """Refuses tensors (name, tensor or None, dtype or None for any) off the current GPU or of another dtype."""
-    import torch
-    device = torch.cuda.current_device()
-    for name, t, dtype in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda or t.device.index != device:
-            raise ValueError("%s: %s must be on the current GPU" % (what, name))
-        if dtype is not None and t.dtype != dtype:
+def _new_like(like, stream):
+    if stream is None:
+        return _torch.empty_like(like)
+    with _torch.cuda.stream(stream):
+        return _torch.empty_like(like)
+
+
+def _on_gpu(what, dtype, names, tensors):
+    """Refuses tensors off the current GPU or of another dtype (None: any); absent ones are None."""
+    if _torch is None:
+        _start()
+    device = _current_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != device or (dtype is not None and t.dtype != dtype)):
+            name = names[[u is t for u in tensors].index(True)]
+            if t.get_device() != device:
+                raise ValueError("%s: %s must be on the current GPU" % (what, name))
             raise TypeError("%s: %s must be %s, not %s" % (what, name, dtype, t.dtype))
 
 
 def make_rope_cfg(rot, theta, layout=ROPE_INTERLEAVED, scaling=ROPE_SCALE_NONE, factor=1.0, turns_low=1.0, turns_high=4.0,
                   trained_len=0, magnitude=1.0):
     """Rotary positions of a head's first `rot` elements (rov_rope_cfg)."""
-    return RopeCfg(int(layout), int(rot), int(scaling), int(trained_len), float(theta), float(factor), float(turns_low),
-                   float(turns_high), float(magnitude))
+    return RopeCfg(layout, rot, scaling, trained_len, theta, factor, turns_low, turns_high, magnitude)
 
 
 def rope(cfg, Q, K=None, positions=None, Qo=None, Ko=None, backward=False, stream=None):
     """Q [B,S,H,d] and K [B,S,Hkv,d] turned by their positions (int64 [B,S], [1,S] or [S]; None: 0..S-1) into
     Qo and Ko (new if None; Q and K themselves for in place).  backward: gradients of Q and K from those of the results."""
-    import torch
     B, S, H, d = Q.shape
-    _same("rope", (("Q", Q, None), ("K", K, Q.dtype), ("Qo", Qo, Q.dtype), ("Ko", Ko, Q.dtype), ("positions", positions, torch.int64)))
-    if K is not None and (K.dim() != 4 or K.shape[:2] != Q.shape[:2] or K.shape[3] != d):
-        raise ValueError("rope: K must be [B, S, Hkv, d] beside Q [B, S, H, d]")
-    if K is None and Ko is not None:
-        raise ValueError("rope: Ko without K")
+    _on_gpu("rope", Q.dtype, ("Q", "K", "Qo", "Ko"), (Q, K, Qo, Ko))
     if Qo is None:
-        Qo = _new(Q.shape, Q.dtype, Q.device, stream)
-    if K is not None and Ko is None:
-        Ko = _new(K.shape, K.dtype, K.device, stream)
-    if Qo.shape != Q.shape or (K is not None and Ko.shape != K.shape):
-        raise ValueError("rope: results have the shapes of Q and K")
-    st = []
-    for name, t in (("Q", Q), ("Qo", Qo), ("K", K), ("Ko", Ko)):
-        if t is None:
-            st += [0, 0, 0]
-            continue
-        if t.stride(3) != 1 and d > 1:
-            raise ValueError("rope: the head dimension of %s must be contiguous" % name)
-        st += t.stride()[:3]
+        Qo = _new_like(Q, stream)
+    elif Qo.shape != Q.shape:
+        raise ValueError("rope: Qo must have the shape of Q")
+    sq, so = Q.stride(), Qo.stride()
+    inner = sq[3] == 1 and so[3] == 1
+    if K is not None:
+        if K.dim() != 4 or K.shape[0] != B or K.shape[1] != S or K.shape[3] != d:
+            raise ValueError("rope: K must be [B, S, Hkv, d] beside Q [B, S, H, d]")
+        Hkv = K.shape[2]
+        if Ko is None:
+            Ko = _new_like(K, stream)
+        elif Ko.shape != K.shape:
+            raise ValueError("rope: Ko must have the shape of K")
+        sk, sl = K.stride(), Ko.stride()
+        inner = inner and sk[3] == 1 and sl[3] == 1
+        kp, kop = K.data_ptr(), Ko.data_ptr()
+    elif Ko is not None:
+        raise ValueError("rope: Ko without K")
+    else:
+        Hkv, sk, sl, kp, kop = 0, (0, 0, 0), (0, 0, 0), None, None
+    if not inner and d > 1:
+        raise ValueError("rope: the head dimension must be contiguous")
     pos, pstride = None, 0
     if positions is not None:
-        positions = positions[None] if positions.dim() == 1 else positions
-        if positions.dim() != 2 or positions.shape[1] != S or positions.shape[0] not in (1, B) or (S > 1 and positions.stride(1) != 1):
+        _on_gpu("rope", _torch.int64, ("positions",), (positions,))
+        shape, ps = positions.shape, positions.stride()
+        if len(shape) not in (1, 2) or shape[-1] != S or (len(shape) == 2 and shape[0] != B and shape[0] != 1) or (S > 1 and ps[-1] != 1):
             raise ValueError("rope: positions must be [B, S], [1, S] or [S], contiguous along S")
-        pos, pstride = positions.data_ptr(), positions.stride(0) if positions.shape[0] > 1 else 0
-    _check(load().rov_rope(ctypes.byref(cfg), Q.data_ptr(), Qo.data_ptr(), K.data_ptr() if K is not None else None,
-                           Ko.data_ptr() if K is not None else None, B, S, H, K.shape[2] if K is not None else 0, d, _I64x12(*st),
-                           _dtype_code(Q), pos, pstride, int(bool(backward)), _stream_ptr(stream)), "rov_rope")
+        pos, pstride = positions.data_ptr(), ps[0] if len(shape) == 2 and shape[0] > 1 else 0
+    _check(load().rov_rope(cfg, Q.data_ptr(), Qo.data_ptr(), kp, kop, B, S, H, Hkv, d,
+                           _pack12(sq[0], sq[1], sq[2], so[0], so[1], so[2], sk[0], sk[1], sk[2], sl[0], sl[1], sl[2]),
+                           _dtype_code(Q), pos, pstride, 1 if backward else 0, _stream_ptr(stream)), "rov_rope")
     return (Qo, Ko) if K is not None else Qo
 
 
-def _rows(what, name, t, n):
-    """(tensor as [rows, n], row stride)"""
-    if t.dim() < 1 or t.shape[-1] != n or (n > 1 and t.stride(-1) != 1):
-        raise ValueError("%s: %s must have %d contiguous columns" % (what, name, n))
-    if t.dim() != 2:
-        if not t.is_contiguous():
-            raise ValueError("%s: %s with %d dimensions must be contiguous" % (what, name, t.dim()))
-        return t.numel() // n, n
-    return t.shape[0], t.stride(0) if t.shape[0] > 1 else n
+def _row_strides(what, names, tensors, shape, n):
+    """Row strides of tensors of one shape [..., n] (n for absent ones)."""
+    out = []
+    for t in tensors:
+        if t is None or t.is_contiguous():
+            if t is not None and t.shape != shape:
+                raise ValueError("%s: %s must be %s" % (what, names[[u is t for u in tensors].index(True)], list(shape)))
+            out.append(n)
+            continue
+        if t.shape != shape or len(shape) != 2 or (n > 1 and t.stride(1) != 1):
+            raise ValueError("%s: %s must be %s with contiguous rows" % (what, names[[u is t for u in tensors].index(True)], list(shape)))
+        out.append(t.stride(0) if shape[0] > 1 else n)
+    return out
 
 
-def _vectors(what, rows, n, w_pre, w_post, gate):
-    for name, t in (("w_pre", w_pre), ("w_post", w_post)):
-        if t is not None and (t.shape != (n,) or not t.is_contiguous()):
-            raise ValueError("%s: %s must be [%d], contiguous" % (what, name, n))
+def _rows_per_gate(what, rows, n, w_pre, w_post, gate):
+    for t in (w_pre, w_post):
+        if t is not None and (t.numel() != n or t.dim() != 1 or not t.is_contiguous()):
+            raise ValueError("%s: weights must be [%d], contiguous" % (what, n))
     if gate is None:
         return rows
-    if gate.shape[-1] != n or gate.dim() > 2 or not gate.is_contiguous():
-        raise ValueError("%s: gate must be [%d] or [gates, %d], contiguous" % (what, n, n))
     gates = gate.numel() // n
-    if gates == 0 or rows % gates:
-        raise ValueError("%s: %d rows do not share %d gates" % (what, rows, gates))
+    if gate.shape[-1] != n or gate.dim() > 2 or not gate.is_contiguous() or gates == 0 or rows % gates:
+        raise ValueError("%s: gate must be [%d] or [gates, %d], contiguous, its gates shared evenly by the %d rows" % (what, n, n, rows))
     return rows // gates
 
 
@@ -653,31 +680,26 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
+
 def norm_residual(x, h, w_pre=None, w_post=None, gate=None, x_scale=1.0, h_scale=1.0, eps=1e-5, y=None, yn=None, yn_fp8_scale=None,
                   stream=None):
     """(y, yn): y = x_scale * x + h_scale * gate * (RMS(h) * w_post), yn = RMS(y) * w_pre (None without w_pre); x, h [..., n],
     gate [n] or [gates, n] (consecutive rows share a gate).  yn_fp8_scale: yn in e4m3 bytes with that scale."""
-    import torch
-    n, dt = x.shape[-1], x.dtype
-    _same("norm_residual", (("x", x, None), ("h", h, dt), ("w_pre", w_pre, dt), ("w_post", w_post, dt), ("gate", gate, dt), ("y", y, dt),
-                            ("yn", yn, dt if yn_fp8_scale is None else torch.uint8)))
+    shape = x.shape
+    n = shape[-1]
+    _on_gpu("norm_residual", x.dtype, ("x", "h", "w_pre", "w_post", "gate", "y"), (x, h, w_pre, w_post, gate, y))
     if y is None:
-        y = _new(x.shape, dt, x.device, stream)
-    if yn is None and w_pre is not None:
-        yn = _new(x.shape, dt if yn_fp8_scale is None else torch.uint8, x.device, stream)
-    rows, ldx = _rows("norm_residual", "x", x, n)
-    ld = [ldx]
-    for name, t in (("h", h), ("y", y), ("yn", yn)):
-        if t is None:
-            ld.append(n)
-            continue
-        if t.shape != x.shape:
-            raise ValueError("norm_residual: %s must have the shape of x" % name)
-        ld.append(_rows("norm_residual", name, t, n)[1])
-    per = _vectors("norm_residual", rows, n, w_pre, w_post, gate)
+        y = _new_like(x, stream)
+    if yn is not None:
+        _on_gpu("norm_residual", x.dtype if yn_fp8_scale is None else _torch.uint8, ("yn",), (yn,))
+    elif w_pre is not None:
+        yn = _new_like(x, stream) if yn_fp8_scale is None else _new(shape, x, stream, _torch.uint8)
+    ld = _row_strides("norm_residual", ("x", "h", "y", "yn"), (x, h, y, yn), shape, n)
+    rows = x.numel() // n
+    per = _rows_per_gate("norm_residual", rows, n, w_pre, w_post, gate)
     _check(load().rov_norm_residual(x.data_ptr(), h.data_ptr(), _ptr(w_post), _ptr(gate), _ptr(w_pre), y.data_ptr(), _ptr(yn), rows, n,
-                                    (_i64 * 4)(*ld), per, _dtype_code(x), float(x_scale), float(h_scale), float(eps),
-                                    float(yn_fp8_scale or 0.0), _stream_ptr(stream)), "rov_norm_residual")
+                                    _pack4(*ld), per, _dtype_code(x), x_scale, h_scale, eps, yn_fp8_scale or 0.0, _stream_ptr(stream)),
+           "rov_norm_residual")
     return y, yn
 
 
@@ -689,37 +711,34 @@ def norm_residual_bwd(y, h, dy, dn=None, w_pre=None, w_post=None, gate=None, x_s
                       workspace=None, stream=None):
     """(dx, dh, dw_pre, dw_post, dgate) of norm_residual from its y and h and the gradients of y (dy, may be None) and yn (dn);
     the last three in fp32, None without their input."""
-    import torch
     like = dy if dy is not None else dn
     if like is None:
         raise ValueError("norm_residual_bwd: dy or dn is needed")
-    n, dt, dev = like.shape[-1], like.dtype, like.device
-    _same("norm_residual_bwd", (("y", y, dt), ("h", h, dt), ("dy", dy, dt), ("dn", dn, dt), ("w_pre", w_pre, dt), ("w_post", w_post, dt),
-                                ("gate", gate, dt), ("dx", dx, dt), ("dh", dh, dt), ("workspace", workspace, None)))
+    shape, dt = like.shape, like.dtype
+    n = shape[-1]
+    names, tensors = ("y", "h", "dy", "dn", "dx", "dh"), (y, h, dy, dn, dx, dh)
+    _on_gpu("norm_residual_bwd", dt, names + ("w_pre", "w_post", "gate"), tensors + (w_pre, w_post, gate))
     if dx is None:
-        dx = _new(like.shape, dt, dev, stream)
+        dx = _new_like(like, stream)
     if dh is None:
-        dh = _new(like.shape, dt, dev, stream)
-    rows, ld = _rows("norm_residual_bwd", "dy", like, n)[0], []
-    for name, t in (("y", y), ("h", h), ("dy", dy), ("dn", dn), ("dx", dx), ("dh", dh)):
-        if t is None:
-            ld.append(n)
-            continue
-        if t.shape != like.shape:
-            raise ValueError("norm_residual_bwd: %s must have the shape of the gradients" % name)
-        ld.append(_rows("norm_residual_bwd", name, t, n)[1])
-    per = _vectors("norm_residual_bwd", rows, n, w_pre, w_post, gate)
-    dw_pre = _new((n,), torch.float32, dev, stream) if w_pre is not None else None
-    dw_post = _new((n,), torch.float32, dev, stream) if w_post is not None else None
-    dgate = _new(gate.shape, torch.float32, dev, stream) if gate is not None else None
-    code = _dtype_code(like)
-    if workspace is None and (dw_pre is not None or dw_post is not None or dgate is not None):
-        workspace = _new((max(1, norm_residual_bwd_workspace_bytes(rows, n, per, code)),), torch.uint8, dev, stream)
-    _check(load().rov_norm_residual_bwd(_ptr(y), _ptr(h), _ptr(w_post), _ptr(gate), _ptr(w_pre), _ptr(dy), _ptr(dn), dx.data_ptr(),
-                                        dh.data_ptr(), _ptr(dw_post), _ptr(dgate), _ptr(dw_pre), rows, n, (_i64 * 6)(*ld), per, code,
-                                        float(x_scale), float(h_scale), float(eps), _ptr(workspace),
-                                        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream_ptr(stream)),
-           "rov_norm_residual_bwd")
+        dh = _new_like(like, stream)
+    ld = _row_strides("norm_residual_bwd", names, (y, h, dy, dn, dx, dh), shape, n)
+    rows = like.numel() // n
+    per = _rows_per_gate("norm_residual_bwd", rows, n, w_pre, w_post, gate)
+    f32 = _torch.float32
+    dw_pre = _new((n,), like, stream, f32) if w_pre is not None else None
+    dw_post = _new((n,), like, stream, f32) if w_post is not None else None
+    dgate = _new(gate.shape, like, stream, f32) if gate is not None else None
+    code, L = _dtype_code(like), load()
+    if workspace is None:
+        size = L.rov_norm_residual_bwd_workspace_bytes(rows, n, per, code) if dw_pre is not None or dw_post is not None or dgate is not None else 0
+        workspace = _new((size,), like, stream, _torch.uint8) if size else None
+    else:
+        _on_gpu("norm_residual_bwd", None, ("workspace",), (workspace,))
+        size = workspace.numel() * workspace.element_size()
+    _check(L.rov_norm_residual_bwd(_ptr(y), _ptr(h), _ptr(w_post), _ptr(gate), _ptr(w_pre), _ptr(dy), _ptr(dn), dx.data_ptr(), dh.data_ptr(),
+                                   _ptr(dw_post), _ptr(dgate), _ptr(dw_pre), rows, n, _pack6(*ld), per, code, x_scale, h_scale, eps,
+                                   _ptr(workspace), size, _stream_ptr(stream)), "rov_norm_residual_bwd")
     return dx, dh, dw_pre, dw_post, dgate
 
 
@@ -727,34 +746,40 @@ def linear_xent_workspace_bytes(M, V, K, dtype, backward=False, vocab_piece=0):
     return int(load().rov_linear_xent_workspace_bytes(int(M), int(V), int(K), int(dtype), int(bool(backward)), int(vocab_piece)))
 
 
-def _xent_operands(what, X, W, rows, *more):
-    import torch
+def _xent_operands(what, X, W, targets, f32, outs):
+    """Checks what both calls take; (M, V, K, row strides of X, W and the results)."""
     if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[1]:
         raise ValueError("%s: X must be [M, K] and W [V, K]" % what)
-    _same(what, (("X", X, None), ("W", W, X.dtype)) + tuple((n, t, torch.int64 if n == "targets" else torch.float32) for n, t in rows) + more)
-    for name, t in rows:
-        if t is not None and (t.shape != (X.shape[0],) or not t.is_contiguous()):
+    (M, K), V = X.shape, W.shape[0]
+    _on_gpu(what, X.dtype, ("X", "W", "dX", "dW"), (X, W) + outs)
+    _on_gpu(what, _torch.int64, ("targets",), (targets,))
+    _on_gpu(what, _torch.float32, tuple(f32), tuple(f32.values()))
+    for name, t in (("targets", targets),) + tuple(f32.items()):
+        if t is not None and (t.shape != (M,) or not t.is_contiguous()):
             raise ValueError("%s: %s must be [M], contiguous" % (what, name))
-    lds = []
-    for name, t in (("X", X), ("W", W)) + tuple((n, t) for n, t, _ in more if n in ("dX", "dW")):
-        lds.append(X.shape[1] if t is None else _rows(what, name, t, X.shape[1])[1])
-    return lds
+    ldx, lddx = _row_strides(what, ("X", "dX"), (X, outs[0] if outs else None), X.shape, K)
+    ldw, lddw = _row_strides(what, ("W", "dW"), (W, outs[1] if outs else None), W.shape, K)
+    return M, V, K, ldx, ldw, lddx, lddw
+
+
+def _xent_workspace(what, workspace, X, stream, *sizes):
+    if workspace is None:
+        return _new((load().rov_linear_xent_workspace_bytes(*sizes),), X, stream, _torch.uint8)
+    _on_gpu(what, None, ("workspace",), (workspace,))
+    return workspace
 
 
 def linear_xent(X, W, targets, scale=1.0, ignore_index=-100, loss=None, lse=None, vocab_piece=0, workspace=None, stream=None):
     """(loss, lse), fp32 [M], of the logits scale * X @ W^T (X [M, K], W [V, K]) against targets (int64 [M])."""
-    import torch
-    ldx, ldw = _xent_operands("linear_xent", X, W, (("targets", targets), ("loss", loss), ("lse", lse)), ("workspace", workspace, None))
-    M, K = X.shape
-    V = W.shape[0]
+    M, V, K, ldx, ldw, _, _ = _xent_operands("linear_xent", X, W, targets, dict(loss=loss, lse=lse), ())
     if loss is None:
-        loss = _new((M,), torch.float32, X.device, stream)
+        loss = _new((M,), X, stream, _torch.float32)
     if lse is None:
-        lse = _new((M,), torch.float32, X.device, stream)
-    if workspace is None:
-        workspace = _new((max(1, linear_xent_workspace_bytes(M, V, K, _dtype_code(X), False, vocab_piece)),), torch.uint8, X.device, stream)
-    _check(load().rov_linear_xent(X.data_ptr(), W.data_ptr(), targets.data_ptr(), M, V, K, ldx, ldw, _dtype_code(X), float(scale),
-                                  int(ignore_index), loss.data_ptr(), lse.data_ptr(), int(vocab_piece), workspace.data_ptr(),
+        lse = _new((M,), X, stream, _torch.float32)
+    code = _dtype_code(X)
+    workspace = _xent_workspace("linear_xent", workspace, X, stream, M, V, K, code, 0, vocab_piece)
+    _check(load().rov_linear_xent(X.data_ptr(), W.data_ptr(), targets.data_ptr(), M, V, K, ldx, ldw, code, scale, ignore_index,
+                                  loss.data_ptr(), lse.data_ptr(), vocab_piece, workspace.data_ptr(),
                                   workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "rov_linear_xent")
     return loss, lse
 
@@ -762,24 +787,17 @@ def linear_xent(X, W, targets, scale=1.0, ignore_index=-100, loss=None, lse=None
 def linear_xent_bwd(X, W, targets, lse, dloss, dlse=None, scale=1.0, ignore_index=-100, dX=None, dW=None, need_dX=True, need_dW=True,
                     vocab_piece=0, workspace=None, stream=None):
     """(dX, dW) from linear_xent's lse and the gradients of loss and lse (fp32 [M]); None for one that is not needed."""
-    import torch
+    M, V, K, ldx, ldw, lddx, lddw = _xent_operands("linear_xent_bwd", X, W, targets, dict(lse=lse, dloss=dloss, dlse=dlse), (dX, dW))
     if dX is None and need_dX:
-        dX = _new(X.shape, X.dtype, X.device, stream)
+        dX = _new((M, K), X, stream, X.dtype)
     if dW is None and need_dW:
-        dW = _new(W.shape, W.dtype, W.device, stream)
-    ldx, ldw, lddx, lddw = _xent_operands("linear_xent_bwd", X, W, (("targets", targets), ("lse", lse), ("dloss", dloss), ("dlse", dlse)),
-                                          ("dX", dX, X.dtype), ("dW", dW, X.dtype), ("workspace", workspace, None))
-    for name, t, like in (("dX", dX, X), ("dW", dW, W)):
-        if t is not None and t.shape != like.shape:
-            raise ValueError("linear_xent_bwd: %s must have the shape of %s" % (name, name[1:]))
-    M, K = X.shape
-    V = W.shape[0]
-    if workspace is None:
-        workspace = _new((max(1, linear_xent_workspace_bytes(M, V, K, _dtype_code(X), True, vocab_piece)),), torch.uint8, X.device, stream)
+        dW = _new((V, K), W, stream, W.dtype)
+    code = _dtype_code(X)
+    workspace = _xent_workspace("linear_xent_bwd", workspace, X, stream, M, V, K, code, 1, vocab_piece)
     _check(load().rov_linear_xent_bwd(X.data_ptr(), W.data_ptr(), targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(), _ptr(dlse), M, V, K,
-                                      ldx, ldw, _dtype_code(X), float(scale), int(ignore_index), _ptr(dX), _ptr(dW), lddx, lddw,
-                                      int(vocab_piece), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                      _stream_ptr(stream)), "rov_linear_xent_bwd")
+                                      ldx, ldw, code, scale, ignore_index, _ptr(dX), _ptr(dW), lddx, lddw, vocab_piece,
+                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "rov_linear_xent_bwd")
     return dX, dW
 
 

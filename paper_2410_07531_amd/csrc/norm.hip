@@ -153,10 +153,10 @@ struct NormBwdParams {
 // whole groups (blockIdx.x, blockIdx.x + gridDim.x, ...), and keeps the column sums of its rows in registers.
 // Row sums: the sum behind dh's mean is linear in g, so its three parts are summed beside mean(y^2), mean(y t) and
 // mean(h^2) and one barrier a row is enough (two sets of scratch by the parity of the row).
-// With one piece a thread the next row is on its way while a row is worked on, and the weights stay in registers.
+// With at most eight elements a thread the next row is on its way while a row is worked on, and the weights stay in registers.
 template <typename T, int W, int NT, int VPT, bool WHOLE>
-__global__ __launch_bounds__(NT, VPT == 1 ? 4 : 1) void norm_bwd_kernel(const NormBwdParams p) {
-    constexpr bool AHEAD = VPT == 1;
+__global__ __launch_bounds__(NT, VPT * W <= 8 ? 4 : 1) void norm_bwd_kernel(const NormBwdParams p) {
+    constexpr bool AHEAD = VPT * W <= 8;
     __shared__ float red[2][6 * 16];
     __builtin_amdgcn_s_setprio(3);
     float col_h[VPT][W], col_y[VPT][W], col_g[WHOLE ? VPT : 1][W];
@@ -186,23 +186,30 @@ __global__ __launch_bounds__(NT, VPT == 1 ? 4 : 1) void norm_bwd_kernel(const No
             }
         }
     };
-    Piece<T, W> ones, kept_pre, kept_post, kept_gate;
+    Piece<T, W> ones, kept_pre[AHEAD ? VPT : 1], kept_post[AHEAD ? VPT : 1], kept_gate[AHEAD ? VPT : 1];
     {
         float f[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) f[j] = 1.0f;
         ones.set(f);
     }
-    kept_pre = kept_post = kept_gate = ones;
-    // a weight or gate of this thread's columns (ones without it): kept in registers where the row is one piece
-    auto vec = [&](const Piece<T, W>& kept, const void* base, int e) {
-        Piece<T, W> v = AHEAD ? kept : ones;
-        if (!AHEAD && base != nullptr) v.load((const T*)base + e);
+    // a weight or gate of this thread's columns (ones without it)
+    auto keep = [&](Piece<T, W>* kept, const T* base) {
+#pragma unroll
+        for (int c = 0; c < VPT; ++c) {
+            const int e = (c * NT + (int)threadIdx.x) * W;
+            kept[c] = ones;
+            if (base != nullptr && e < p.n) kept[c].load(base + e);
+        }
+    };
+    auto vec = [&](const Piece<T, W>* kept, const void* base, int c) {
+        Piece<T, W> v = AHEAD ? kept[c] : ones;
+        if (!AHEAD && base != nullptr) v.load((const T*)base + (c * NT + (int)threadIdx.x) * W);
         return v;
     };
-    if (AHEAD && (int)threadIdx.x * W < p.n) {
-        if (has_pre) kept_pre.load((const T*)p.w_pre + threadIdx.x * W);
-        if (has_post) kept_post.load((const T*)p.w_post + threadIdx.x * W);
+    if constexpr (AHEAD) {
+        keep(kept_pre, (const T*)p.w_pre);
+        keep(kept_post, (const T*)p.w_post);
     }
     int parity = 0;
     for (int group = WHOLE ? (int)blockIdx.x : (int)blockIdx.x / p.chunks; group < p.groups; group += WHOLE ? (int)gridDim.x : p.groups) {
@@ -213,7 +220,7 @@ __global__ __launch_bounds__(NT, VPT == 1 ? 4 : 1) void norm_bwd_kernel(const No
             r0 += len * chunk / p.chunks;
         }
         const T* const gate = p.gate != nullptr ? (const T*)p.gate + (int64_t)group * p.n : nullptr;
-        if (AHEAD && gate != nullptr && (int)threadIdx.x * W < p.n) kept_gate.load(gate + threadIdx.x * W);
+        if constexpr (AHEAD) keep(kept_gate, gate);
         Row cur, next;
         if (AHEAD && r0 < r1) fetch(next, r0);
         for (int64_t row = r0; row < r1; ++row) {
@@ -228,7 +235,7 @@ __global__ __launch_bounds__(NT, VPT == 1 ? 4 : 1) void norm_bwd_kernel(const No
             for (int c = 0; c < VPT; ++c) {
                 const int e = (c * NT + (int)threadIdx.x) * W;
                 if (e >= p.n) continue;
-                const Piece<T, W> w = vec(kept_pre, p.w_pre, e), wp = vec(kept_post, p.w_post, e), g = vec(kept_gate, gate, e);
+                const Piece<T, W> w = vec(kept_pre, p.w_pre, c), wp = vec(kept_post, p.w_post, c), g = vec(kept_gate, gate, c);
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
                     const float y = cur.y[c].at(j), h = cur.h[c].at(j), t = cur.dn[c].at(j) * w.at(j), u = h * wp.at(j) * g.at(j);
@@ -251,7 +258,7 @@ __global__ __launch_bounds__(NT, VPT == 1 ? 4 : 1) void norm_bwd_kernel(const No
             for (int c = 0; c < VPT; ++c) {
                 const int e = (c * NT + (int)threadIdx.x) * W;
                 if (e >= p.n) continue;
-                const Piece<T, W> w = vec(kept_pre, p.w_pre, e), wp = vec(kept_post, p.w_post, e), g = vec(kept_gate, gate, e);
+                const Piece<T, W> w = vec(kept_pre, p.w_pre, c), wp = vec(kept_post, p.w_post, c), g = vec(kept_gate, gate, c);
                 float dx[W], dh[W];
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
@@ -316,55 +323,74 @@ struct NormSumParams {
     int whole;
 };
 
-// Column sums of the workgroups' partial sums: 64 columns a workgroup, 16 threads a column.
-template <typename T>
+// Column sums of the workgroups' partial sums: 16 columns a workgroup, 64 threads a column.  BY_GROUP (many gates): a thread adds up whole
+// groups; else a column's threads share the rows of each group.
+template <typename T, bool BY_GROUP>
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const NormSumParams p) {
-    __shared__ float red[16][64];
-    const int col = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    __shared__ float red[2][16][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = blockIdx.x * 16 + (lane & 15), slice = wave * 4 + (lane >> 4);
     const bool in = col < p.n;
-    auto column = [&](const float* part, int first, int count) {
+    int parity = 0;
+    auto strided = [&](const float* part, int64_t first, int count, int from, int step) {
         float s = 0.0f;
         if (in)
-#pragma unroll 4
-            for (int i = slice; i < count; i += 16) s += part[(int64_t)(first + i) * p.n + col];
-        red[slice][threadIdx.x & 63] = s;
-        __syncthreads();
-        if (slice == 0)
-#pragma unroll
-            for (int i = 1; i < 16; ++i) s += red[i][threadIdx.x & 63];
-        __syncthreads();
+#pragma unroll 8
+            for (int i = from; i < count; i += step) s += part[(first + i) * p.n + col];
         return s;
     };
+    // every thread's s, summed over a column's 64 threads
+    auto over_column = [&](float s) {
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (lane < 16) red[parity][wave][lane] = s;
+        __syncthreads();
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += red[parity][i][lane & 15];
+        parity ^= 1;   // (the next sum's scratch: this one may still be read)
+        return s;
+    };
+    auto gate_of = [&](int64_t g) {
+        float f[1];
+        load_or<T, 1>(p.gate != nullptr ? (const T*)p.gate + g * p.n : nullptr, col, f, 1.0f);
+        return f[0];
+    };
+    const bool writes = slice == 0 && in;
     if (p.dw_pre != nullptr) {
-        const float s = column(p.part_y, 0, p.parts);
-        if (slice == 0 && in) p.dw_pre[col] = s;
+        const float s = over_column(strided(p.part_y, 0, p.parts, slice, 64));
+        if (writes) p.dw_pre[col] = s;
     }
     if (p.part_h == nullptr) return;
-    float wp = 1.0f, total = 0.0f;
-    if (in) {
-        float f[1];
-        load_or<T, 1>(p.w_post, col, f, 1.0f);
-        wp = f[0];
-    }
-    for (int g = 0; g < p.groups; ++g) {
-        const float s = column(p.part_h, g * p.chunks, p.chunks);
-        if (slice != 0 || !in) continue;
-        float f[1] = {1.0f};
-        if (!p.whole) {
-            load_or<T, 1>(p.gate != nullptr ? (const T*)p.gate + (int64_t)g * p.n : nullptr, col, f, 1.0f);
-            if (p.dgate != nullptr) p.dgate[(int64_t)g * p.n + col] = p.h_scale * wp * s;
+    float wp[1] = {1.0f}, total = 0.0f;
+    if (in) load_or<T, 1>(p.w_post, col, wp, 1.0f);
+    if constexpr (BY_GROUP) {
+        if (in)
+            for (int g = slice; g < p.groups; g += 64) {
+                const float s = strided(p.part_h, (int64_t)g * p.chunks, p.chunks, 0, 1);
+                if (p.dgate != nullptr) p.dgate[(int64_t)g * p.n + col] = p.h_scale * wp[0] * s;
+                total = __builtin_fmaf(gate_of(g), s, total);
+            }
+        if (p.dw_post == nullptr) return;
+        total = over_column(total);
+    } else {
+        for (int g = 0; g < p.groups; ++g) {
+            const float s = over_column(strided(p.part_h, (int64_t)g * p.chunks, p.chunks, slice, 64));
+            if (!writes) continue;
+            if (p.dgate != nullptr) p.dgate[(int64_t)g * p.n + col] = p.h_scale * wp[0] * s;
+            total = __builtin_fmaf(p.whole ? 1.0f : gate_of(g), s, total);
         }
-        total = __builtin_fmaf(f[0], s, total);
     }
-    if (slice == 0 && in && p.dw_post != nullptr) p.dw_post[col] = p.h_scale * total;
+    if (writes && p.dw_post != nullptr) p.dw_post[col] = p.h_scale * total;
 }
 
-// Threads of a workgroup and pieces a thread for a row of `pieces` pieces.
+// Threads of a workgroup and pieces a thread for a row of `pieces` pieces of w elements: one piece a thread, or four single elements.
 struct RowShape { int nt, vpt; };
-RowShape row_shape(int pieces) {
+RowShape row_shape(int pieces, int w) {
     if (pieces <= 64) return {64, 1};
     if (pieces <= 128) return {128, 1};
     if (pieces <= 256) return {256, 1};
+    if (w == 1 && pieces <= 1024) return {256, 4};
     if (pieces <= 512) return {512, 1};
     if (pieces <= 1024) return {1024, 1};
     if (pieces <= 4096) return {1024, 4};
@@ -373,48 +399,63 @@ RowShape row_shape(int pieces) {
 
 template <typename T, int W, bool OUT8>
 void launch_fwd(const NormParams& p, hipStream_t stream) {
-    const RowShape s = row_shape((p.n + W - 1) / W);
+    const RowShape s = row_shape((p.n + W - 1) / W, W);
     const dim3 grid((unsigned)p.rows);
 #define ROV_FWD(NT, VPT) hipLaunchKernelGGL((norm_fwd_kernel<T, W, NT, VPT, OUT8>), grid, dim3(NT), 0, stream, p)
     if (s.nt == 64) ROV_FWD(64, 1);
     else if (s.nt == 128) ROV_FWD(128, 1);
-    else if (s.nt == 256) ROV_FWD(256, 1);
-    else if (s.nt == 512) ROV_FWD(512, 1);
-    else if (s.vpt == 1) ROV_FWD(1024, 1);
-    else if (W > 4 || s.vpt == 4) ROV_FWD(1024, 4);
-    else if constexpr (W <= 4) ROV_FWD(1024, (W == 1 ? 32 : 8));
+    else if (s.nt == 256 && s.vpt == 1) ROV_FWD(256, 1);
+    else if constexpr (W == 1) {
+        if (s.nt == 256) ROV_FWD(256, 4);
+        else if (s.vpt == 4) ROV_FWD(1024, 4);
+        else ROV_FWD(1024, 32);
+    } else {
+        if (s.nt == 512) ROV_FWD(512, 1);
+        else if (s.vpt == 1) ROV_FWD(1024, 1);
+        else if (W == 8 || s.vpt == 4) ROV_FWD(1024, 4);
+        else if constexpr (W == 4) ROV_FWD(1024, 8);
+    }
 #undef ROV_FWD
 }
 
 template <typename T, int W, bool WHOLE>
 void launch_bwd(const NormBwdParams& p, int blocks, hipStream_t stream) {
-    const RowShape s = row_shape((p.n + W - 1) / W);
+    const RowShape s = row_shape((p.n + W - 1) / W, W);
     const dim3 grid((unsigned)blocks);
 #define ROV_BWD(NT, VPT) hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, VPT, WHOLE>), grid, dim3(NT), 0, stream, p)
     if (s.nt == 64) ROV_BWD(64, 1);
     else if (s.nt == 128) ROV_BWD(128, 1);
-    else if (s.nt == 256) ROV_BWD(256, 1);
-    else if (s.nt == 512) ROV_BWD(512, 1);
-    else if (s.vpt == 1) ROV_BWD(1024, 1);
-    else if (W > 4 || s.vpt == 4) ROV_BWD(1024, 4);
-    else if constexpr (W <= 4) ROV_BWD(1024, (W == 1 ? 32 : 8));
+    else if (s.nt == 256 && s.vpt == 1) ROV_BWD(256, 1);
+    else if constexpr (W == 1) {
+        if (s.nt == 256) ROV_BWD(256, 4);
+        else if (s.vpt == 4) ROV_BWD(1024, 4);
+        else ROV_BWD(1024, 32);
+    } else {
+        if (s.nt == 512) ROV_BWD(512, 1);
+        else if (s.vpt == 1) ROV_BWD(1024, 1);
+        else if (W == 8 || s.vpt == 4) ROV_BWD(1024, 4);
+        else if constexpr (W == 4) ROV_BWD(1024, 8);
+    }
 #undef ROV_BWD
 }
 
 // How the rows are shared: `blocks` workgroups, `chunks` of them a group of rows with one gate, or (whole) every
 // workgroup takes whole groups.
 struct RowSplit { int blocks, chunks; bool whole; };
-RowSplit split_rows(int64_t rows, int64_t rows_per_gate, int pieces) {
-    const int64_t groups = rows / rows_per_gate;
-    const int64_t most = (int64_t)device_cu_count() * (1024 / row_shape(pieces).nt);
-    int64_t want = rows / 4 < 1 ? 1 : rows / 4;
+RowSplit split_rows(int64_t rows, int64_t rows_per_gate, int n, int dtype) {
+    const int w = dtype == ROV_F32 ? (n % 4 == 0 ? 4 : 1) : n % 8 == 0 ? 8 : 1;
+    const int64_t groups = rows / rows_per_gate, ncu = device_cu_count();
+    // a workgroup a compute unit where each gets two rows (few rows wait for their loads: 1003 x 1001 in fp32 with 250 workgroups 15 us); more only
+    // with eight rows each, so that the partial sums stay a fraction of the rows' bytes
+    const int64_t most = ncu * (1024 / row_shape(n / w, w).nt);
+    int64_t want = rows / 8 < ncu ? (rows / 2 < ncu ? rows / 2 : ncu) : rows / 8;
     if (want > most) want = most;
+    if (want < 1) want = 1;
     if (groups > want) return {(int)want, 1, true};
     int64_t chunks = want / groups;
     if (chunks > rows_per_gate) chunks = rows_per_gate;
     return {(int)(groups * chunks), (int)chunks, false};
 }
-int row_pieces(int n, int dtype) { return dtype == ROV_F32 ? (n % 4 == 0 ? n / 4 : n) : (n % 8 == 0 ? n / 8 : n); }
 
 int check_norm_sizes(int64_t rows, int n, int64_t rows_per_gate, int dtype, float x_scale, float h_scale, float eps) {
     if (rows <= 0 || n <= 0 || rows_per_gate <= 0 || rows % rows_per_gate != 0) return ROV_ERR_INVALID;
@@ -480,7 +521,7 @@ extern "C" int rov_norm_residual(const void* x, const void* h, const void* w_pos
 extern "C" size_t rov_norm_residual_bwd_workspace_bytes(int64_t rows, int n, int64_t rows_per_gate, int dtype) {
     if (rov::check_norm_sizes(rows, n, rows_per_gate, dtype, 1.0f, 1.0f, 1.0f) != ROV_OK) return 0;
     // (the split of rows off 16 bytes, with a thread an element, has no more workgroups)
-    return 2 * sizeof(float) * (size_t)n * (size_t)rov::split_rows(rows, rows_per_gate, rov::row_pieces(n, dtype)).blocks;
+    return 2 * sizeof(float) * (size_t)n * (size_t)rov::split_rows(rows, rows_per_gate, n, dtype).blocks;
 }
 
 extern "C" int rov_norm_residual_bwd(const void* y, const void* h, const void* w_post, const void* gate, const void* w_pre,
@@ -512,7 +553,7 @@ extern "C" int rov_norm_residual_bwd(const void* y, const void* h, const void* w
     for (const void* q : vectors) vec = vec && aligned(q, 16);
     for (int i = 0; i < 6; ++i)
         if (tensors[i] != nullptr) vec = vec && aligned(tensors[i], 16) && ld[i] % w == 0;
-    const RowSplit sp = split_rows(rows, rows_per_gate, row_pieces(n, dtype));
+    const RowSplit sp = split_rows(rows, rows_per_gate, n, dtype);
     const bool sums = sums_h || dw_pre != nullptr;
     if (sums) {
         if (workspace == nullptr || !aligned(workspace, 16)) return ROV_ERR_INVALID;
@@ -535,9 +576,14 @@ extern "C" int rov_norm_residual_bwd(const void* y, const void* h, const void* w
     if (!sums) return ROV_OK;
     NormSumParams s{p.part_h, p.part_y, w_post, gate, dw_post, sp.whole ? nullptr : dgate, dw_pre, n, sp.blocks,
                     sp.whole ? 1 : p.groups, sp.whole ? sp.blocks : sp.chunks, h_scale, sp.whole ? 1 : 0};
-    const dim3 grid((unsigned)((n + 63) / 64));
-    if (dtype == ROV_F32) hipLaunchKernelGGL((norm_sum_kernel<float>), grid, dim3(1024), 0, st, s);
-    else hipLaunchKernelGGL((norm_sum_kernel<uint16_t>), grid, dim3(1024), 0, st, s);
+    const dim3 grid((unsigned)((n + 15) / 16)), block(1024);
+    if (s.groups >= 16) {
+        if (dtype == ROV_F32) hipLaunchKernelGGL((norm_sum_kernel<float, true>), grid, block, 0, st, s);
+        else hipLaunchKernelGGL((norm_sum_kernel<uint16_t, true>), grid, block, 0, st, s);
+    } else {
+        if (dtype == ROV_F32) hipLaunchKernelGGL((norm_sum_kernel<float, false>), grid, block, 0, st, s);
+        else hipLaunchKernelGGL((norm_sum_kernel<uint16_t, false>), grid, block, 0, st, s);
+    }
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }

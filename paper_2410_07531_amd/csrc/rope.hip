@@ -4,8 +4,9 @@
 //
 // Pair p of a head, (a, b), at position s becomes m * (a cos t - b sin t, a sin t + b cos t), t = s * f_p.
 // What bounds it: memory, every element read and written once.  The sines of a token serve all its heads, so a
-// workgroup owns TPB tokens, forms their rot / 2 sines once into LDS and then walks over the heads, 16 bytes
-// a thread.
+// workgroup owns a few tokens, forms their rot / 2 sines once into LDS and then walks over the heads, 16 bytes
+// a thread.  16384 x (32 + 8) heads x 128 in bf16: 69 us, 4.9 TB/s, the rate of a large copy; 16 tokens of it 4.5 us, the chain of position, sines
+// and store.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -27,16 +28,21 @@ struct RopeParams {
     int64_t positions_stride;
     int64_t tokens;
     int S, H, heads;             // heads = H + Hkv
-    int d, rot, copy;            // copy: elements behind `rot` go along (0 in place)
-    double log2_theta, inv_factor, low, inv_width, turns;   // turns: trained_len / (2 pi)
+    int rot, copy, tpb;          // copy: elements behind `rot` that go along (0 in place); tpb: tokens a workgroup
+    uint32_t units, token_units, inv_units, inv_token_units;   // of a head, of a token
+    double power[8];             // theta^(-2 * 2^k / rot)
+    double inv_factor, low, inv_width, turns;   // turns: trained_len / (2 pi)
     int scaling;
     float magnitude, sign;
 };
 
 // Sine and cosine of position * frequency(p).  The angle is formed and reduced modulo 2 pi in double, so that
-// positions of a million keep fp32-accurate sines.
+// positions of a million keep fp32-accurate sines.  The frequency is a product of powers theta^(-2 * 2^k / rot), one
+// per bit of the pair's number, that the host worked out: at most eight products in place of an exponential in double.
 __device__ __forceinline__ void rope_sincos(const RopeParams& p, int64_t pos, int pair, float* sn, float* cs) {
-    double f = exp2(-2.0 * (double)pair / (double)p.rot * p.log2_theta);
+    double f = 1.0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f *= (pair >> k) & 1 ? p.power[k] : 1.0;
     if (p.scaling == ROV_ROPE_SCALE_LINEAR) f *= p.inv_factor;
     if (p.scaling == ROV_ROPE_SCALE_PARTS) {
         double keep = (p.turns * f - p.low) * p.inv_width;
@@ -51,92 +57,122 @@ __device__ __forceinline__ void rope_sincos(const RopeParams& p, int64_t pos, in
     *cs = c * p.magnitude;
 }
 
+// n / d by a multiplication where that is exact (inv = 2^32 / d rounded up, n * d < 2^32), else inv == 0
+__device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t inv) { return inv != 0 ? __umulhi(n, inv) : n / d; }
+
 // W: elements a thread moves at once (16 bytes), or 1 where rows, heads or `rot` are off 16 bytes.
-// A unit of a head is W pairs (split layout: W elements of each half), max(1, W / 2) pairs (adjacent), or W elements to copy.
-template <typename T, int W, bool HALVES, int TPB>
+// A unit of a head is W pairs (split layout: W elements of each half), max(1, W / 2) pairs (adjacent), or W elements to copy; a
+// workgroup's units are those of all heads of its tokens.  A thread loads two units before it waits for anything, the first two
+// before the sines are formed.
+template <typename T, int W, bool HALVES>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
-    extern __shared__ __attribute__((aligned(16))) float lds[];   // [TPB][rot / 2] sines, then cosines
-    const int half = p.rot / 2;
+    extern __shared__ __attribute__((aligned(16))) float lds[];   // [tokens][rot / 2] sines, then cosines
+    constexpr int AHEAD = 2;
+    constexpr bool TWO = HALVES || W == 1;                 // a unit's pairs lie in two pieces
+    constexpr int P = HALVES ? W : (W > 1 ? W / 2 : 1);    // pairs of a unit
+    const int half = p.rot / 2, turn_units = half / P;
     float* const sines = lds;
-    float* const cosines = lds + TPB * half;
+    float* const cosines = lds + p.tpb * half;
     // beside a co-resident RNG grid the waves would wait for issue slots behind its long integer multiplies
     __builtin_amdgcn_s_setprio(3);
-    const int64_t token0 = (int64_t)blockIdx.x * TPB;
-    for (int i = threadIdx.x; i < TPB * half; i += 256) {
-        const int tk = i / half;
-        const int64_t token = token0 + tk;
-        if (token >= p.tokens) break;
-        const int64_t b = token / p.S, s = token - b * p.S;
-        const int64_t pos = p.positions != nullptr ? p.positions[b * p.positions_stride + s] : s;
-        rope_sincos(p, pos, i - tk * half, &sines[i], &cosines[i]);
-    }
-    __syncthreads();
-    constexpr int P = HALVES ? W : (W > 1 ? W / 2 : 1);    // pairs of a unit
-    const int turn_units = half / P, units = turn_units + p.copy / W;
-    for (int tk = 0; tk < TPB; ++tk) {
-        const int64_t token = token0 + tk;
-        if (token >= p.tokens) return;
-        const int64_t b = token / p.S, s = token - b * p.S;
-        for (int i = threadIdx.x; i < p.heads * units; i += 256) {
-            const int head = i / units, u = i - head * units;
-            const int k = head >= p.H;
-            const int hh = k ? head - p.H : head;
-            const T* src = (const T*)p.src[k] + b * p.sb[k] + s * p.ss[k] + (int64_t)hh * p.sh[k];
-            T* dst = (T*)p.dst[k] + b * p.db[k] + s * p.ds[k] + (int64_t)hh * p.dh[k];
-            if (u >= turn_units) {
-                const int e = p.rot + (u - turn_units) * W;
-                Piece<T, W> v;
-                v.load(src + e);
-                v.store(dst + e);
+    const int64_t token0 = (int64_t)blockIdx.x * p.tpb;
+    const int here = p.tokens - token0 < p.tpb ? (int)(p.tokens - token0) : p.tpb;
+    const uint32_t total = (uint32_t)here * p.token_units;
+    const int64_t b0 = token0 / p.S;
+    const uint32_t s0 = (uint32_t)(token0 - b0 * p.S);
+    const bool one_row = s0 + (uint32_t)here <= (uint32_t)p.S;   // (one sequence holds the workgroup's tokens)
+    for (uint32_t base = 0; base < total; base += 256 * AHEAD) {
+        Piece<T, W> va[AHEAD], vb[AHEAD];
+        T* dst[AHEAD];
+        int unit[AHEAD], at[AHEAD];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            const uint32_t i = base + q * 256 + threadIdx.x;
+            unit[q] = -1;
+            if (i >= total) continue;
+            const uint32_t tk = quotient(i, p.token_units, p.inv_token_units), in_token = i - tk * p.token_units;
+            const uint32_t head = quotient(in_token, p.units, p.inv_units);
+            unit[q] = (int)(in_token - head * p.units);
+            at[q] = (int)tk * half + unit[q] * P;
+            const uint32_t over = one_row ? 0 : (s0 + tk) / (uint32_t)p.S;
+            const int64_t b = b0 + over, s = s0 + tk - over * (uint32_t)p.S;
+            const int k = (int)head >= p.H, hh = k ? (int)head - p.H : (int)head;
+            const T* const src = (const T*)p.src[k] + b * p.sb[k] + s * p.ss[k] + (int64_t)hh * p.sh[k];
+            dst[q] = (T*)p.dst[k] + b * p.db[k] + s * p.ds[k] + (int64_t)hh * p.dh[k];
+            if (unit[q] >= turn_units) {
+                va[q].load(src + p.rot + (unit[q] - turn_units) * W);
+            } else if constexpr (TWO) {
+                va[q].load(src + (HALVES ? unit[q] * W : 2 * unit[q]));
+                vb[q].load(src + (HALVES ? half + unit[q] * W : 2 * unit[q] + 1));
+            } else {
+                va[q].load(src + unit[q] * W);
+            }
+        }
+        if (base == 0) {
+            for (int i = threadIdx.x; i < here * half; i += 256) {
+                const int tk = i / half;
+                const uint32_t over = one_row ? 0 : (s0 + (uint32_t)tk) / (uint32_t)p.S;
+                const int64_t b = b0 + over, s = s0 + (uint32_t)tk - over * (uint32_t)p.S;
+                const int64_t pos = p.positions != nullptr ? p.positions[b * p.positions_stride + s] : s;
+                rope_sincos(p, pos, i - tk * half, &sines[i], &cosines[i]);
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            if (unit[q] < 0) continue;
+            if (unit[q] >= turn_units) {
+                va[q].store(dst[q] + p.rot + (unit[q] - turn_units) * W);
                 continue;
             }
-            const float* sn = sines + tk * half + u * P;
-            const float* cs = cosines + tk * half + u * P;
-            if constexpr (HALVES || W == 1) {
-                // split pairs; one element of each also serves adjacent pairs off 16 bytes
-                const int ea = HALVES ? u * W : 2 * u, eb = HALVES ? half + u * W : 2 * u + 1;
-                Piece<T, W> va, vb;
-                va.load(src + ea);
-                vb.load(src + eb);
-                float a[W], c[W];
-                va.get(a);
-                vb.get(c);
+            const float* const sn = sines + at[q];
+            const float* const cs = cosines + at[q];
+            float a[W];
+            va[q].get(a);
+            if constexpr (TWO) {
+                float c[W];
+                vb[q].get(c);
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
                     const float x = a[j], y = c[j];
                     a[j] = x * cs[j] - y * sn[j];
                     c[j] = x * sn[j] + y * cs[j];
                 }
-                va.set(a);
-                vb.set(c);
-                va.store(dst + ea);
-                vb.store(dst + eb);
+                va[q].set(a);
+                vb[q].set(c);
+                va[q].store(dst[q] + (HALVES ? unit[q] * W : 2 * unit[q]));
+                vb[q].store(dst[q] + (HALVES ? half + unit[q] * W : 2 * unit[q] + 1));
             } else {
-                Piece<T, W> v;
-                v.load(src + u * W);
-                float a[W];
-                v.get(a);
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
                     const float x = a[2 * j], y = a[2 * j + 1];
                     a[2 * j] = x * cs[j] - y * sn[j];
                     a[2 * j + 1] = x * sn[j] + y * cs[j];
                 }
-                v.set(a);
-                v.store(dst + u * W);
+                va[q].set(a);
+                va[q].store(dst[q] + unit[q] * W);
             }
         }
     }
 }
 
 template <typename T, int W, bool HALVES>
-int launch_form(const RopeParams& p, hipStream_t stream) {
-    // four tokens a workgroup while that still fills the chip eightfold
-    const int tpb = p.tokens >= (int64_t)device_cu_count() * 32 ? 4 : 1;
+int launch_form(RopeParams& p, hipStream_t stream) {
+    const int pairs = HALVES ? W : (W > 1 ? W / 2 : 1);
+    const int64_t units = p.rot / 2 / pairs + p.copy / W, token_units = units * p.heads;
+    if (token_units > 0x0FFFFFFF) return ROV_ERR_UNSUPPORTED;
+    p.units = (uint32_t)units;
+    p.token_units = (uint32_t)token_units;
+    // tokens a workgroup: a sine for every thread, as long as three workgroups a compute unit are left
+    int tpb = 1;
+    while (tpb * p.rot <= 256 && p.tokens >= (int64_t)device_cu_count() * 6 * tpb) tpb *= 2;
+    p.tpb = tpb;
+    auto inverse = [&](int64_t n, int64_t d) { return n * d < ((int64_t)1 << 32) && d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0u; };
+    p.inv_token_units = inverse(tpb * token_units, token_units);
+    p.inv_units = inverse(token_units, units);
     const int64_t blocks = (p.tokens + tpb - 1) / tpb;
     if (blocks > 0x7FFFFFFF) return ROV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((tpb == 4 ? rope_kernel<T, W, HALVES, 4> : rope_kernel<T, W, HALVES, 1>), dim3((unsigned)blocks), dim3(256),
-                       (size_t)tpb * p.rot * sizeof(float), stream, p);
+    hipLaunchKernelGGL((rope_kernel<T, W, HALVES>), dim3((unsigned)blocks), dim3(256), (size_t)tpb * p.rot * sizeof(float), stream, p);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
@@ -198,8 +234,9 @@ int launch_rope_cfg(const rov_rope_cfg* c, const void* Q, void* Qo, const void* 
     p.positions = positions; p.positions_stride = positions_stride;
     p.tokens = (int64_t)B * S;
     p.S = S; p.H = H; p.heads = H + Hkv;
-    p.d = d; p.rot = c->rot; p.copy = copy ? d - c->rot : 0;
-    p.log2_theta = log2((double)c->theta);
+    p.rot = c->rot; p.copy = copy ? d - c->rot : 0;
+    p.power[0] = exp2(-2.0 / (double)c->rot * log2((double)c->theta));
+    for (int k = 1; k < 8; ++k) p.power[k] = p.power[k - 1] * p.power[k - 1];
     p.scaling = c->scaling;
     p.inv_factor = c->scaling == ROV_ROPE_SCALE_NONE ? 1.0 : 1.0 / (double)c->factor;
     if (c->scaling == ROV_ROPE_SCALE_PARTS) {
