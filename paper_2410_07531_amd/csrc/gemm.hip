@@ -299,15 +299,16 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     for (int j = 0; j < 8; ++j) {
         const int row = (wave + 4 * j) * 8 + (lane >> 3);
         const int chunk = (lane & 7) ^ swz(row);
-        // HEAD_GRAD: LDS row 128*h + 16*i + r holds activation row 128*h + 8*r + i and weight row 128*h + 16*j + 4*g + e weight row
-        // 128*h + 32*g + 4*j + e, so that a lane ends up with eight consecutive rows and 32 consecutive columns of the tile
+        // HEAD_GRAD: LDS row 128*h + 16*i + r holds activation row 128*h + 8*r + i, and weight row 128*h + 32*j + 16*k + 4*g + e (k = 0, 1) weight
+        // row 128*h + 32*j + 8*g + 4*k + e, so that a lane ends up with eight consecutive rows and four times eight consecutive columns of the
+        // tile, and the four lanes of a row with 32
         const int arow = HEAD == HEAD_GRAD ? (row & 128) | ((row & 15) << 3) | ((row >> 4) & 7) : row;
         const int ra = arow < rows_a ? arow : rows_a - 1;   // rows past the edge are never stored
         // dual: LDS rows [16*NJ*h, +8*NJ) are gate rows of output columns 8*NJ*h .., the next 8*NJ the up rows;
         // mixed: LDS rows [16*b, +8) are gate rows of output columns 8*b .., the next 8 the up rows
         const int wcol = MIXED ? (row >> 4) * 8 + (row & 7)
                                : DUAL ? (row / (16 * NJ)) * (8 * NJ) + row % (8 * NJ) : row;
-        const int wrow = HEAD == HEAD_GRAD ? (row & 128) | (((row >> 2) & 3) << 5) | (((row >> 4) & 7) << 2) | (row & 3) : wcol;
+        const int wrow = HEAD == HEAD_GRAD ? (row & (128 + 64 + 32)) | (((row >> 2) & 3) << 3) | (((row >> 4) & 1) << 2) | (row & 3) : wcol;
         const int rw = wrow < rows_w ? wrow : rows_w - 1;
         voff_a[j] = (uint32_t)((size_t)ra * ld_a) + (uint32_t)(chunk * 16);
         if (j < NJ) voff_w[j] = (uint32_t)((size_t)rw * ld_w) + (uint32_t)(chunk * 16);
@@ -554,37 +555,46 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         // gradients of the logits, G[m][n] and its transpose; rows that are ignored or beyond M and columns beyond N are zero, so that
         // both can be walked in whole slots as the next products' k
         const int mw = m0 + wm * 128 + 8 * mrow;          // first of this lane's eight rows
-        const int nl = n0 + wn * 128 + 8 * nsub;          // first of its 32 columns
+        const int nl = n0 + wn * 128 + 2 * nsub;          // first of its columns nl + 32*j + 0..7
         float lse2[8], up[8], down[8];
         int tcol[8];
-        bool keep[8];
+        bool keep[8], whole = n0 + wn * 128 + 128 <= N, hit = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int m = mw + i;
             const int64_t t = m < M ? head.targets[m] : head.ignore;
             keep[i] = t != head.ignore;
+            whole = whole && keep[i];
             const float a = keep[i] ? (t >= 0 && t < head.vocab ? head.dloss[m] : NAN) : 0.0f;
             const float b = keep[i] && head.dlse != nullptr ? head.dlse[m] : 0.0f;
             lse2[i] = keep[i] ? head.lse[m] * 1.44269504088896341f : 0.0f;
             up[i] = (a + b) * head.scale;
             down[i] = a * head.scale;
-            const int64_t c = t - head.v0 - nl;
-            tcol[i] = keep[i] && c >= 0 && c < 32 ? (int)c : -1;
+            const int64_t c = t - head.v0 - nl;   // 32*j + 0..7: this lane's
+            tcol[i] = keep[i] && c >= 0 && c < 128 && (c & 31) < 8 ? (int)c : -1;
+            hit = hit || tcol[i] >= 0;
         }
+        // most waves see neither an ignored row, nor an edge, nor a target
+        const bool plain = __ballot(!whole || hit) == 0;
 #pragma unroll
         for (int jj = 0; jj < NJ; jj += 2) {
             __builtin_amdgcn_sched_barrier(0);
-            float g[8][8];   // [row][column 4*jj + c]
+            const int n = nl + 16 * jj;
+            float g[8][8];   // [row][column n + c]
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc_read(acc[jj + (c >> 2)][i][c & 3]), alpha, -lse2[i]));
-                    float q = p * up[i];
-                    if (tcol[i] == 4 * jj + c) q -= down[i];
-                    g[i][c] = keep[i] && nl + 4 * jj + c < N ? q : 0.0f;
-                }
-            const int n = nl + 4 * jj;
+                for (int c = 0; c < 8; ++c)
+                    g[i][c] = up[i] * __builtin_amdgcn_exp2f(__builtin_fmaf(acc_read(acc[jj + (c >> 2)][i][c & 3]), alpha, -lse2[i]));
+            if (!plain) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        if (tcol[i] == 16 * jj + c) g[i][c] -= down[i];
+                        if (!keep[i] || n + c >= N) g[i][c] = 0.0f;
+                    }
+            }
             if (head.g != nullptr && n < head.ld_g)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
