@@ -611,46 +611,57 @@ def make_rope_cfg(rot, theta, layout=ROPE_INTERLEAVED, scaling=ROPE_SCALE_NONE, 
 def rope(cfg, Q, K=None, positions=None, Qo=None, Ko=None, backward=False, stream=None):
     """Q [B,S,H,d] and K [B,S,Hkv,d] turned by their positions (int64 [B,S], [1,S] or [S]; None: 0..S-1) into
     Qo and Ko (new if None; Q and K themselves for in place).  backward: gradients of Q and K from those of the results."""
-    B, S, H, d = Q.shape
+    B, S, H, d = shape = Q.shape
     _on_gpu("rope", Q.dtype, ("Q", "K", "Qo", "Ko"), (Q, K, Qo, Ko))
     if Qo is None:
         Qo = _new_like(Q, stream)
-    elif Qo.shape != Q.shape:
+    elif Qo.shape != shape:
         raise ValueError("rope: Qo must have the shape of Q")
-    sq, so = Q.stride(), Qo.stride()
-    inner = sq[3] == 1 and so[3] == 1
+    q0, q1, q2, qd = Q.stride()
+    o0, o1, o2, od = Qo.stride()
+    inner = qd == 1 == od
     if K is not None:
-        if K.dim() != 4 or K.shape[0] != B or K.shape[1] != S or K.shape[3] != d:
+        kshape = K.shape
+        if len(kshape) != 4 or kshape[0] != B or kshape[1] != S or kshape[3] != d:
             raise ValueError("rope: K must be [B, S, Hkv, d] beside Q [B, S, H, d]")
-        Hkv = K.shape[2]
+        Hkv = kshape[2]
         if Ko is None:
             Ko = _new_like(K, stream)
-        elif Ko.shape != K.shape:
+        elif Ko.shape != kshape:
             raise ValueError("rope: Ko must have the shape of K")
-        sk, sl = K.stride(), Ko.stride()
-        inner = inner and sk[3] == 1 and sl[3] == 1
+        k0, k1, k2, kd = K.stride()
+        l0, l1, l2, ld = Ko.stride()
+        inner = inner and kd == 1 == ld
         kp, kop = K.data_ptr(), Ko.data_ptr()
     elif Ko is not None:
         raise ValueError("rope: Ko without K")
     else:
-        Hkv, sk, sl, kp, kop = 0, (0, 0, 0), (0, 0, 0), None, None
+        Hkv = k0 = k1 = k2 = l0 = l1 = l2 = 0
+        kp = kop = None
     if not inner and d > 1:
         raise ValueError("rope: the head dimension must be contiguous")
     pos, pstride = None, 0
     if positions is not None:
         _on_gpu("rope", _torch.int64, ("positions",), (positions,))
         shape, ps = positions.shape, positions.stride()
-        if len(shape) not in (1, 2) or shape[-1] != S or (len(shape) == 2 and shape[0] != B and shape[0] != 1) or (S > 1 and ps[-1] != 1):
+        if (shape != (B, S) and shape != (1, S) and shape != (S,)) or (S > 1 and ps[-1] != 1):
             raise ValueError("rope: positions must be [B, S], [1, S] or [S], contiguous along S")
-        pos, pstride = positions.data_ptr(), ps[0] if len(shape) == 2 and shape[0] > 1 else 0
+        pos = positions.data_ptr()
+        if len(shape) == 2 and shape[0] > 1:
+            pstride = ps[0]
     _check(load().rov_rope(cfg, Q.data_ptr(), Qo.data_ptr(), kp, kop, B, S, H, Hkv, d,
-                           _pack12(sq[0], sq[1], sq[2], so[0], so[1], so[2], sk[0], sk[1], sk[2], sl[0], sl[1], sl[2]),
+                           _pack12(q0, q1, q2, o0, o1, o2, k0, k1, k2, l0, l1, l2),
                            _dtype_code(Q), pos, pstride, 1 if backward else 0, _stream_ptr(stream)), "rov_rope")
     return (Qo, Ko) if K is not None else Qo
 
 
 def _row_strides(what, names, tensors, shape, n):
     """Row strides of tensors of one shape [..., n] (n for absent ones)."""
+    for t in tensors:
+        if t is not None and not (t.is_contiguous() and t.shape == shape):
+            break
+    else:
+        return (n,) * len(tensors)
     out = []
     for t in tensors:
         if t is None or t.is_contiguous():
@@ -671,6 +682,8 @@ def _rows_per_gate(what, rows, n, w_pre, w_post, gate):
     if gate is None:
         return rows
     gates = gate.numel() // n
+    if gate.shape == (n,) and gate.is_contiguous():
+        return rows
     if gate.shape[-1] != n or gate.dim() > 2 or not gate.is_contiguous() or gates == 0 or rows % gates:
         raise ValueError("%s: gate must be [%d] or [gates, %d], contiguous, its gates shared evenly by the %d rows" % (what, n, n, rows))
     return rows // gates

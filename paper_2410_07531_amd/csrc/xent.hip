@@ -211,6 +211,7 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const float* __restrict_
 }
 
 constexpr size_t kAlign = 256;
+int64_t up_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 size_t up(size_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
 
 // Columns of a piece: at most 256 MiB of fp32 logits, in whole tiles.
@@ -243,15 +244,15 @@ XentLayout layout(int M, int V, int K, int asked, bool backward) {
     return l;
 }
 
-// Columns of a piece of the bf16 backward pass: G and its transpose are 128 MiB each at most, the piece of W transposed 32768 columns.
-int piece_cols_bf16(int M, int V, int asked) {
-    int64_t p = asked > 0 ? asked : ((int64_t)64 << 20) / M;
-    p = asked > 0 ? (p + 255) / 256 * 256 : p / 256 * 256 < 1024 ? 1024 : p / 256 * 256;
-    if (asked <= 0 && p > 32768) p = 32768;
+// Columns of a piece of the bf16 backward pass: G, its transpose and the piece of W transposed take at most 128 MiB each (8192 x
+// 131072 x 4096: 16 pieces).
+int piece_cols_bf16(int M, int V, int K, int asked) {
+    const int64_t wide = M > K ? M : K;
+    int64_t p = asked > 0 ? up_to(asked, 256) : ((int64_t)64 << 20) / wide / 256 * 256;
+    if (asked <= 0 && p < 1024) p = 1024;
     return p > V ? V : (int)p;
 }
 constexpr int kPackCols = 4096;   // columns of W that the forward pass packs at a time, where it has to
-int64_t up_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Workgroups that share a 256 x 256 tile's k in the products for dX and dW: enough to cover the compute units, at
 // least eight slots (512 values of k) each.
@@ -281,7 +282,7 @@ HeadLayout head_layout(int M, int V, int K, int asked, bool backward) {
         l.part = take((size_t)(2 * gemm_head_tiles_n(V) + 2) * M * sizeof(float2));
         l.picked = take((size_t)M * 4);
     } else {
-        l.piece = piece_cols_bf16(M, V, asked);
+        l.piece = piece_cols_bf16(M, V, K, asked);
         const int64_t pp = up_to(l.piece, 64);
         l.shares_x = shares_of(M, K, pp);
         l.shares_w = shares_of(l.piece, K, l.mp);
