@@ -155,6 +155,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef i32x2 i32x2_u __attribute__((aligned(4)));   // stored to rows that start on 4 bytes
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4* lds_i16x4_ptr;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -213,7 +215,9 @@ __device__ __forceinline__ void epilogue_combine(int epi, uint2 r, float& c0, fl
 // RAGGED: rows of any multiple of 16 bytes (k ends inside the last slot: its lanes beyond k are aimed outside the operands,
 // one select a load, and read zeros) and any number of output columns.
 // HEAD: the products of the loss over the vocabulary (HeadArgs; bf16, rows of any stride): the epilogue keeps the row statistics of
-// the tile's logits (HEAD_STATS), or the gradients of its logits (HEAD_GRAD), or adds the tile to fp32 sums (HEAD_SUM).
+// the tile's logits (HEAD_STATS), or the gradients of its logits (HEAD_GRAD), or stores or adds up fp32 sums (HEAD_DX, HEAD_DW).
+// HEAD_DX: the second operand lies as [K, N] (rows of k), HEAD_DW: both do.  Such an operand's part of a slot is 64 rows of k by 256
+// columns; fragments come by the transposing LDS load, two a fragment, with the k order of the other operand's.
 template <int NJ, bool FP8, bool DUAL = false, bool OUT8 = false, bool RAGGED = false, int HEAD = 0>
 __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char* __restrict__ Wt,
                                           const char* __restrict__ Wt2, uint16_t* __restrict__ C,
@@ -222,7 +226,7 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
                                           const int wave, float alpha2 = 1.0f, float out_inv = 1.0f,
                                           const HeadArgs& head = HeadArgs{}) {
     static_assert(!OUT8 || DUAL, "e4m3 output exists in the dual form only");
-    static_assert(HEAD == 0 || (!FP8 && !DUAL && (HEAD != HEAD_GRAD || NJ == 8)), "the loss's products: plain bf16");
+    static_assert(HEAD == 0 || (!FP8 && !DUAL && (HEAD <= HEAD_STATS || NJ == 8)), "the loss's products: plain bf16, 256 columns");
     static_assert(!RAGGED || (!FP8 && !DUAL), "rows off 128 bytes: the plain bf16 product only");
     constexpr bool MIXED = DUAL && NJ % 4 != 0;   // gate and up rows in every weight block
     const int wm = wave >> 1, wn = wave & 1;
@@ -282,16 +286,22 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     // Loads: wave w issues row blocks (8 rows) w, w+4, ... of each operand: 8 + NJ instructions
     // per slot.  Lane L fills physical chunk L%8 of row L/8, i.e. fetches logical chunk (L%8) ^ swz(row).
     const size_t ld_bytes = (size_t)K * ESZ;
-    int ns = (int)((ld_bytes + (RAGGED ? kRow - 1 : 0)) / kRow);   // slots to walk
-    if constexpr (HEAD == HEAD_SUM) {   // this workgroup's share of k
+    constexpr bool KNW = HEAD == HEAD_DX || HEAD == HEAD_DW, KNA = HEAD == HEAD_DW;
+    int ns = (int)((ld_bytes + (RAGGED || KNW ? kRow - 1 : 0)) / kRow);   // slots to walk
+    const size_t ld_a = HEAD ? head.ld_a : ld_bytes, ld_w = HEAD ? head.ld_w : ld_bytes;
+    int k_rows = 0;             // rows of k from this workgroup's share on
+    if constexpr (KNW) {
         const int s0 = (int)((int64_t)ns * blockIdx.y / gridDim.y), s1 = (int)((int64_t)ns * (blockIdx.y + 1) / gridDim.y);
         ns = s1 - s0;
-        A += (size_t)s0 * kRow;
-        Wt += (size_t)s0 * kRow;
+        k_rows = K - s0 * 64;
+        A += KNA ? (size_t)s0 * 64 * ld_a : (size_t)s0 * kRow;
+        Wt += (size_t)s0 * 64 * ld_w;
     }
-    const size_t ld_a = HEAD ? head.ld_a : ld_bytes, ld_w = HEAD ? head.ld_w : ld_bytes;
     // bytes of k that a row holds from the base on (the last row's end bounds the operand)
-    const size_t k_bytes = HEAD == HEAD_SUM ? (size_t)ns * kRow : ld_bytes;
+    const size_t k_bytes = KNW ? (size_t)ns * kRow : ld_bytes;
+    // 16-byte chunk swizzle of an LDS row of 256 columns: lanes that the transposing load serves together read rows {0-3, 8-11} (+4, +16) x 32
+    // bytes, so the 32-byte groups of those rows have to differ
+    auto swz_kn = [](int row) { return ((row & 3) | (((row >> 3) & 1) << 2)) << 1; };
     const int rows_a = M - m0 < BM ? M - m0 : BM;
     const int rows_w = N - n0 < BNT ? N - n0 : BNT;
     uint32_t voff_a[8], voff_w[NJ];
@@ -312,9 +322,15 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         const int rw = wrow < rows_w ? wrow : rows_w - 1;
         voff_a[j] = (uint32_t)((size_t)ra * ld_a) + (uint32_t)(chunk * 16);
         if (j < NJ) voff_w[j] = (uint32_t)((size_t)rw * ld_w) + (uint32_t)(chunk * 16);
+        if constexpr (KNW) {   // a load is two rows of k
+            const int krow = (wave + 4 * j) * 2 + (lane >> 5);
+            const uint32_t at = (uint32_t)(((lane & 31) ^ swz_kn(krow)) * 16);
+            if (KNA) voff_a[j] = (uint32_t)krow * (uint32_t)ld_a + at;
+            voff_w[j] = (uint32_t)krow * (uint32_t)ld_w + at;
+        }
     }
-    const char* a_panel = A + (size_t)m0 * ld_a;
-    const char* w_panel = Wt + (size_t)n0 * ld_w;
+    const char* a_panel = A + (KNA ? (size_t)m0 * ESZ : (size_t)m0 * ld_a);
+    const char* w_panel = Wt + (KNW ? (size_t)n0 * ESZ : (size_t)n0 * ld_w);
     // slot at which this workgroup starts its cyclic walk over k (the sum does not depend on the
     // order; the fp32 rounding does, deterministically)
     const int kstart = (int)((unsigned)tm % (unsigned)ns);
@@ -329,10 +345,12 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         r[3] = 0x00020000;
         return r;
     };
-    const i32x4 rsrc_a = make_rsrc(a_panel, HEAD ? (size_t)(rows_a - 1) * ld_a + k_bytes : (size_t)rows_a * ld_bytes);
+    // ([K, N]: up to the last column of the last row of k, in whole chunks, so that rows beyond k read as zeros)
+    auto kn_bytes = [&](size_t ld, int cols) { return (size_t)(k_rows - 1) * ld + (size_t)((cols + 7) / 8 * 16); };
+    const i32x4 rsrc_a = make_rsrc(a_panel, KNA ? kn_bytes(ld_a, M - m0) : HEAD ? (size_t)(rows_a - 1) * ld_a + k_bytes : (size_t)rows_a * ld_bytes);
     // (mixed: a load fills 8 rows, row block wave + 4*j, so odd waves load the up rows)
     const i32x4 rsrc_w = make_rsrc(MIXED && (wave & 1) ? Wt2 + (size_t)n0 * ld_bytes : w_panel,
-                                   HEAD ? (size_t)(rows_w - 1) * ld_w + k_bytes : (size_t)rows_w * ld_bytes);
+                                   KNW ? kn_bytes(ld_w, N - n0) : HEAD ? (size_t)(rows_w - 1) * ld_w + k_bytes : (size_t)rows_w * ld_bytes);
     const i32x4 rsrc_w2 = DUAL && !MIXED ? make_rsrc(Wt2 + (size_t)n0 * ld_bytes, (size_t)rows_w * ld_bytes) : rsrc_w;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lptr_t)lds;
     // RAGGED: does the lane's chunk (the same in every load: row / 2 % 8 does not depend on j) lie beyond k in the last slot?
@@ -347,7 +365,7 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         int st = step < ns ? step : ns - 1;       // past the end: harmless reload of the last slot
         st += kstart;
         st = st >= ns ? st - ns : st;
-        const int koff = st * kRow;
+        const int koff = (q < 8 ? KNA : KNW) ? (int)((uint32_t)st * 64u * (uint32_t)(q < 8 ? ld_a : ld_w)) : st * kRow;
         if (q < 8) {
             const uint32_t dst = slot + (uint32_t)((wave + 4 * q) * 1024);
             const uint32_t vo = RAGGED && st == ns - 1 && beyond_k ? (uint32_t)rsrc_a[2] : voff_a[q];
@@ -431,8 +449,21 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         }
     } else {
         i32x4 af[2][8], wf[2][NJ];   // fragments of the two k-steps of a slot
+        // [K, N] operands: lane 16g + 4r + s supplies rows 32h + 8g (+4) + r, columns 4s of the block, and receives its own column's values
+        const int kn_r = (lane >> 2) & 3, kn_g = lane >> 4;
+        const int kn_lane = (8 * kn_g + kn_r) * 512 + (lane & 3) * 8, kn_f = kn_r | ((kn_g & 1) << 2);
+        auto read_kn = [&](const char* base, int h, int b) {
+            const char* const at = base + kn_lane + ((b ^ kn_f) << 5) + h * 32 * 512;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)at);
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + 4 * 512));
+            return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
         auto read_frag = [&](int h, const char* slot, int f /*0..7 = A block, 8..7+NJ = W block*/) {
-            if (f < 8)
+            if (KNA && f < 8)
+                af[h][f] = read_kn(slot + wm * 256, h, f);
+            else if (KNW && f >= 8)
+                wf[h][f - 8] = read_kn(slot + BM * kRow + wn * 256, h, f - 8);
+            else if (f < 8)
                 af[h][f] = *reinterpret_cast<const i32x4*>(slot + a_base + f * 16 * kRow + foff[h]);
             else
                 wf[h][f - 8] = *reinterpret_cast<const i32x4*>(slot + w_base + (f - 8) * 16 * kRow + foff[h]);
@@ -552,8 +583,8 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         return;
     }
     if constexpr (HEAD == HEAD_GRAD) {
-        // gradients of the logits, G[m][n] and its transpose; rows that are ignored or beyond M and columns beyond N are zero, so that
-        // both can be walked in whole slots as the next products' k
+        // gradients of the logits, G[m][n]; rows that are ignored and columns beyond N are zero, so that G can be walked in whole slots as the
+        // next product's k
         const int mw = m0 + wm * 128 + 8 * mrow;          // first of this lane's eight rows
         const int nl = n0 + wn * 128 + 2 * nsub;          // first of its columns nl + 32*j + 0..7
         float lse2[8], up[8], down[8];
@@ -595,24 +626,17 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
                         if (!keep[i] || n + c >= N) g[i][c] = 0.0f;
                     }
             }
-            if (head.g != nullptr && n < head.ld_g)
+            if (n < head.ld_g)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (mw + i < M)
                         *reinterpret_cast<uint4*>(head.g + (size_t)(mw + i) * head.ld_g + n) =
                             make_uint4(pack_bf16x2(g[i][0], g[i][1]), pack_bf16x2(g[i][2], g[i][3]), pack_bf16x2(g[i][4], g[i][5]),
                                        pack_bf16x2(g[i][6], g[i][7]));
-            if (head.gt != nullptr && mw < head.ld_gt)
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    if (n + c < N)
-                        *reinterpret_cast<uint4*>(head.gt + (size_t)(n + c) * head.ld_gt + mw) =
-                            make_uint4(pack_bf16x2(g[0][c], g[1][c]), pack_bf16x2(g[2][c], g[3][c]), pack_bf16x2(g[4][c], g[5][c]),
-                                       pack_bf16x2(g[6][c], g[7][c]));
         }
         return;
     }
-    if constexpr (HEAD == HEAD_SUM) {
+    if constexpr (KNW) {
         // fp32 sums of the shares of k, rows of ld_sum values; or the result itself, bf16
         float* const sums = head.sum != nullptr ? head.sum + (size_t)blockIdx.y * M * head.ld_sum : nullptr;
 #pragma unroll
@@ -761,7 +785,7 @@ __global__ __launch_bounds__(256, 1) void gemm_tn_kernel(const char* __restrict_
                        __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
-// The products of the loss over the vocabulary (see gemm_tile, HEAD); HEAD_SUM: gridDim.y shares of k.
+// The products of the loss over the vocabulary (see gemm_tile, HEAD); HEAD_DX, HEAD_DW: gridDim.y shares of k.
 template <int NJ, bool RAGGED, int HEAD>
 __global__ __launch_bounds__(256, 1) void gemm_head_kernel(const char* __restrict__ A, const char* __restrict__ Wt, uint16_t* __restrict__ C,
                                                           int M, int N, int K, float alpha, int tiles_m, int tiles_n, const HeadArgs head) {
@@ -1034,23 +1058,23 @@ int gemm_head_tiles_n(int N) { return (N + BN - 1) / BN; }
 
 int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
                      hipStream_t stream) {
-    const bool ragged = K % 64 != 0;
+    const bool kn = kind == HEAD_DX || kind == HEAD_DW, kna = kind == HEAD_DW, ragged = !kn && K % 64 != 0;
     if (A == nullptr || W == nullptr || M <= 0 || N <= 0 || K <= 0 || shares <= 0 || shares > 65535) return ROV_ERR_INVALID;
-    if (!aligned(A, 16) || !aligned(W, 16) || head.ld_a % 16 != 0 || head.ld_w % 16 != 0 || K % 8 != 0) return ROV_ERR_INVALID;
-    if (head.ld_a < (size_t)K * 2 || head.ld_w < (size_t)K * 2 || (kind == HEAD_SUM && (ragged || shares > K / 64))) return ROV_ERR_INVALID;
-    // a 256-row operand panel is addressed with 32-bit byte offsets
-    if ((unsigned long long)BM * head.ld_a + 1024 > 0xFFFFFFFFull || (unsigned long long)BN * head.ld_w + 1024 > 0xFFFFFFFFull)
+    if (!aligned(A, 16) || !aligned(W, 16) || head.ld_a % 16 != 0 || head.ld_w % 16 != 0 || (!kn && K % 8 != 0)) return ROV_ERR_INVALID;
+    const int64_t slots = ((int64_t)K + 63) / 64;
+    if (head.ld_a < (size_t)(kna ? (M + 7) / 8 * 16 : kn ? slots * kRowBytes : (int64_t)K * 2)) return ROV_ERR_INVALID;
+    if (head.ld_w < (size_t)(kn ? (N + 7) / 8 * 16 : (int64_t)K * 2) || (!kn && shares > 1) || shares > slots) return ROV_ERR_INVALID;
+    // an operand's panel (256 rows, or all rows of k) is addressed with 32-bit byte offsets
+    if ((unsigned long long)(kna ? slots * 64 : BM) * head.ld_a + 1024 > 0xFFFFFFFFull ||
+        (unsigned long long)(kn ? slots * 64 : BN) * head.ld_w + 1024 > 0xFFFFFFFFull)
         return ROV_ERR_UNSUPPORTED;
     typedef void (*kern_t)(const char*, const char*, uint16_t*, int, int, int, float, int, int, const HeadArgs);
-    static const kern_t sum[5] = {gemm_head_kernel<4, false, HEAD_SUM>, gemm_head_kernel<5, false, HEAD_SUM>, gemm_head_kernel<6, false, HEAD_SUM>,
-                                  gemm_head_kernel<7, false, HEAD_SUM>, gemm_head_kernel<8, false, HEAD_SUM>};
-    const int nj = kind == HEAD_SUM && shares == 1 ? best_tile_cols(M, N) / 32 : 8;
     const kern_t kern = kind == HEAD_STATS  ? (ragged ? gemm_head_kernel<8, true, HEAD_STATS> : gemm_head_kernel<8, false, HEAD_STATS>)
                         : kind == HEAD_GRAD ? (ragged ? gemm_head_kernel<8, true, HEAD_GRAD> : gemm_head_kernel<8, false, HEAD_GRAD>)
-                                            : sum[nj - 4];
+                                            : (kna ? gemm_head_kernel<8, false, HEAD_DW> : gemm_head_kernel<8, false, HEAD_DX>);
     const int rc = set_max_dynamic_lds((const void*)kern, kLdsBytes);
     if (rc != ROV_OK) return rc;
-    const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + 32 * nj - 1) / (32 * nj);
+    const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
     if (tiles_m * tiles_n > 0x7FFFFFFFLL) return ROV_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
                        (uint16_t*)C, M, N, K, alpha, (int)tiles_m, (int)tiles_n, head);

@@ -107,16 +107,16 @@ int launch_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, void* 
                            float scaleA, float scaleWg, float scaleWu, float scaleC, hipStream_t stream);
 int check_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, const void* C, int M, int N, int K,
                           float scaleC);
-// The products of the loss over the vocabulary (bf16, fp32 accumulation; A [M,K], W [N,K], K contiguous, K % 8 == 0, strides
-// ld_a, ld_w in bytes, multiples of 16), as forms of the 256-row kernel with other epilogues:
+// The products of the loss over the vocabulary (bf16, fp32 accumulation; strides ld_a, ld_w in bytes, multiples of 16), as forms of the
+// 256-row kernel with other epilogues.  A [M,K], W [N,K], K contiguous, K % 8 == 0:
 //   HEAD_STATS  z = A W^T * alpha (logits in units of log 2): per row and half tile (128 columns) maximum and sum of exp2 to
-//               part[2 * gemm_head_tiles_n(N)][M], the target's z to picked[m] (rows whose target is one of the N columns);
-//   HEAD_GRAD   G[m][n] = scale * (exp2(z - lse log2 e) * (dloss + dlse) - [v0 + n == target] * dloss) in bf16 to g [M][ld_g] and
-//               its transpose to gt [N][ld_gt] (either may be NULL); columns N .. ld_g and rows M .. ld_gt are zero (ld_g, ld_gt: K of the next products,
-//               below the next multiple of 256), rows of ignored targets too;
-//   HEAD_SUM    C or fp32 sums of A W^T, K % 64 == 0: `shares` workgroups a tile take a share of k each and write (add: add to)
-//               sum[share][M][ld_sum]; sum == NULL (one share): bf16 to C, rows of ld_out (out_wide: rows on 8 bytes).
-enum { HEAD_STATS = 1, HEAD_GRAD = 2, HEAD_SUM = 3 };
+//               part[2 * gemm_head_tiles_n(N)][M], the target's z to picked[m] (rows whose target is one of the N columns, v0 the first);
+//   HEAD_GRAD   G[m][n] = scale * (exp2(z - lse log2 e) * (dloss + dlse) - [v0 + n == target] * dloss) in bf16 to g [M][ld_g], columns
+//               N .. ld_g (N rounded up to 64) and rows of ignored targets zero.
+// W [K,N], N contiguous, and A [M,K] with rows of whole slots (64 values, zero beyond K; HEAD_DX) or [K,M] (HEAD_DW): A W or A^T W;
+// `shares` workgroups a tile take a share of k each and write fp32 (add: add to) sum[share][M][ld_sum]; sum == NULL (one share): bf16
+// to C, rows of ld_out (out_wide: rows on 8 bytes).
+enum { HEAD_STATS = 1, HEAD_GRAD = 2, HEAD_DX = 3, HEAD_DW = 4 };
 struct HeadArgs {
     size_t ld_a = 0, ld_w = 0;
     const int64_t* targets = nullptr;
@@ -126,8 +126,7 @@ struct HeadArgs {
     const float* dloss = nullptr;
     const float* dlse = nullptr;
     uint16_t* g = nullptr;
-    uint16_t* gt = nullptr;
-    int64_t ld_g = 0, ld_gt = 0;
+    int64_t ld_g = 0;
     int64_t ignore = 0, v0 = 0, vocab = 0;
     float scale = 1.0f;
     float* sum = nullptr;

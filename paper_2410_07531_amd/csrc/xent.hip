@@ -6,10 +6,9 @@
 //
 // bf16: the 256-row kernel of gemm.hip with its own epilogues.  Forward, a tile's logits are reduced in the accumulators to a
 // maximum and a sum of exponentials per row and 128 columns, which a second kernel joins; nothing else leaves the tile.  Backward
-// walks the vocabulary in pieces: the accumulators of a piece's logits become G, stored in bf16 with k contiguous for either of the next
-// products (G for dX, its transpose for dW; the tile's rows and columns are dealt to the lanes so that both leave in 16-byte stores), and
-// X and the piece of W are transposed once for them.  dX is summed over the pieces, and over shares of the vocabulary where its tiles alone
-// would leave compute units idle, in fp32.
+// walks the vocabulary in pieces: the accumulators of a piece's logits become G, stored in bf16 (the tile's columns are dealt to the lanes so
+// that G leaves in 16-byte stores), and the products for dX and dW read G, W and X as they lie, k across the rows, through transposing LDS
+// loads.  dX is summed over the pieces, and either over shares of k where its tiles alone would leave compute units idle, in fp32.
 // fp32: the fp32 products of gemm_ring.hip; a piece's logits live in the workspace while they are reduced, or turned into G in place.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -113,50 +112,27 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(float* __restrict__ z, f
 }
 
 // ------------------------------------------------------------------ bf16
-// dst [rows][kp] = src, columns K .. kp zero.
-__global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restrict__ src, int64_t ld, uint16_t* __restrict__ dst, int64_t rows, int K, int kp) {
-    const int64_t total = rows * kp;
+// dst [rows][kp] = src, columns K .. kp zero, rows of ignored targets (targets may be NULL) zero; eight values a thread.
+__global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restrict__ src, int64_t ld, uint16_t* __restrict__ dst, int64_t rows, int K, int kp,
+                                                        bool wide, const int64_t* __restrict__ targets, int64_t ignore) {
+    const int chunks = kp / 8;
+    const int64_t total = rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / kp;
-        const int c = (int)(i - r * kp);
-        dst[i] = c < K ? src[r * ld + c] : (uint16_t)0;
-    }
-}
-
-// dst [K][ldt] = src [rows][ld] transposed; rows of ignored targets (targets may be NULL) and columns rows .. ldt are zero.
-// 64 x 64 values a workgroup through LDS, 128 bytes of a row at a time on either side; VEC: src rows on 16 bytes.
-template <bool VEC>
-__global__ __launch_bounds__(256) void xent_transpose_kernel(const uint16_t* __restrict__ src, int64_t ld, uint16_t* __restrict__ dst, int64_t ldt, int rows,
-                                                            int K, const int64_t* __restrict__ targets, int64_t ignore) {
-    __shared__ uint16_t tile[64][66];
-    const int r0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
-    for (int i = threadIdx.x; i < 512; i += 256) {
-        const int r = i >> 3, c = (i & 7) * 8;
+        const int64_t r = i / chunks;
+        const int c = (int)(i - r * chunks) * 8;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        const bool in = r0 + r < rows && !(targets != nullptr && targets[r0 + r] == ignore);
-        const uint16_t* const at = src + (int64_t)(r0 + r) * ld + k0 + c;
-        if (in) {
-            if (VEC && k0 + c + 8 <= K) {
+        if (targets == nullptr || targets[r] != ignore) {
+            const uint16_t* const at = src + r * ld + c;
+            if (wide) {
                 v = *reinterpret_cast<const uint4*>(at);
             } else {
                 uint32_t h[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = k0 + c + e < K ? at[e] : 0u;
+                for (int e = 0; e < 8; ++e) h[e] = c + e < K ? at[e] : 0u;
                 v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
             }
         }
-        uint32_t* const to = reinterpret_cast<uint32_t*>(&tile[r][c]);
-        to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 512; i += 256) {
-        const int k = i >> 3, r = (i & 7) * 8;
-        if (k0 + k >= K || r0 + r >= ldt) continue;
-        uint32_t h[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = tile[r + e][k];
-        *reinterpret_cast<uint4*>(dst + (int64_t)(k0 + k) * ldt + r0 + r) =
-            make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        *reinterpret_cast<uint4*>(dst + r * kp + c) = v;
     }
 }
 
@@ -244,15 +220,17 @@ XentLayout layout(int M, int V, int K, int asked, bool backward) {
     return l;
 }
 
-// Columns of a piece of the bf16 backward pass: G, its transpose and the piece of W transposed take at most 128 MiB each (8192 x
-// 131072 x 4096: 16 pieces).
-int piece_cols_bf16(int M, int V, int K, int asked) {
-    const int64_t wide = M > K ? M : K;
-    int64_t p = asked > 0 ? up_to(asked, 256) : ((int64_t)64 << 20) / wide / 256 * 256;
+// Columns of a piece of the bf16 backward pass: G takes at most 256 MiB.  Columns of W packed at a time, where it has to be: 128 MiB.
+int piece_cols_bf16(int M, int V, int asked) {
+    int64_t p = asked > 0 ? up_to(asked, 256) : ((int64_t)128 << 20) / M / 256 * 256;
     if (asked <= 0 && p < 1024) p = 1024;
     return p > V ? V : (int)p;
 }
-constexpr int kPackCols = 4096;   // columns of W that the forward pass packs at a time, where it has to
+int pack_cols(int V, int64_t kp) {
+    int64_t p = ((int64_t)64 << 20) / kp / 256 * 256;
+    if (p < 1024) p = 1024;
+    return p > V ? V : (int)p;
+}
 
 // Workgroups that share a 256 x 256 tile's k in the products for dX and dW: enough to cover the compute units, at
 // least eight slots (512 values of k) each.
@@ -264,34 +242,31 @@ int shares_of(int M, int N, int64_t K) {
 }
 
 struct HeadLayout {
-    int piece, shares_x, shares_w;
-    int64_t kp, mp, ks;    // K and M as rows of products, K as rows of sums
-    size_t x, w, part, picked, xt, g, gt, sum_x, sum_w, total;
+    int piece, packed, shares_x, shares_w;   // columns of a piece, of a piece of W that is packed
+    int64_t kp, ks;                          // K as rows of packed operands, of sums
+    size_t x, w, part, picked, g, sum_x, sum_w, total;
 };
 HeadLayout head_layout(int M, int V, int K, int asked, bool backward) {
     HeadLayout l{};
     l.kp = up_to(K, 8);
-    l.mp = up_to(M, 64);
     l.ks = up_to(K, 4);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
+    l.packed = pack_cols(V, l.kp);
+    if (backward) {
+        l.piece = piece_cols_bf16(M, V, asked);
+        if (l.packed > l.piece) l.packed = l.piece;
+    }
     l.x = take((size_t)M * l.kp * 2);
+    l.w = take((size_t)l.packed * l.kp * 2);
     if (!backward) {
-        l.piece = V < kPackCols ? V : kPackCols;
-        l.w = take((size_t)l.piece * l.kp * 2);
-        l.part = take((size_t)(2 * gemm_head_tiles_n(V) + 2) * M * sizeof(float2));
+        l.part = take((size_t)2 * gemm_head_tiles_n(V) * M * sizeof(float2));
         l.picked = take((size_t)M * 4);
     } else {
-        l.piece = piece_cols_bf16(M, V, K, asked);
-        const int64_t pp = up_to(l.piece, 64);
-        l.shares_x = shares_of(M, K, pp);
-        l.shares_w = shares_of(l.piece, K, l.mp);
-        const size_t packed = (size_t)l.piece * l.kp * 2, turned = (size_t)K * pp * 2;
-        l.w = take(packed > turned ? packed : turned);   // the piece of W: packed for the logits, then transposed
-        l.xt = take((size_t)K * l.mp * 2);
-        l.g = take((size_t)M * pp * 2);
-        l.gt = take((size_t)l.piece * l.mp * 2);
-        l.sum_x = take(l.shares_x > 1 || l.piece < V ? (size_t)l.shares_x * M * l.ks * 4 : 0);
+        l.shares_x = shares_of(M, K, l.packed);
+        l.shares_w = shares_of(l.packed, K, M);
+        l.g = take((size_t)M * up_to(l.piece, 64) * 2);
+        l.sum_x = take(l.shares_x > 1 || l.packed < V ? (size_t)l.shares_x * M * l.ks * 4 : 0);
         l.sum_w = take(l.shares_w > 1 ? (size_t)l.shares_w * l.piece * l.ks * 4 : 0);
     }
     l.total = at;
@@ -315,25 +290,17 @@ int check_xent(const void* X, const void* W, const int64_t* targets, int M, int 
     return ROV_OK;
 }
 
-int pack(const void* src, int64_t ld, void* dst, int64_t rows, int K, int64_t kp, hipStream_t st) {
-    hipLaunchKernelGGL(xent_pack_kernel, dim3(sweep_grid(rows * kp)), dim3(256), 0, st, (const uint16_t*)src, ld, (uint16_t*)dst, rows, K, (int)kp);
+int pack(const void* src, int64_t ld, void* dst, int64_t rows, int K, int64_t kp, const int64_t* targets, int64_t ignore, hipStream_t st) {
+    const bool wide = K % 8 == 0 && ld % 8 == 0 && aligned(src, 16);
+    hipLaunchKernelGGL(xent_pack_kernel, dim3(sweep_grid(rows * kp / 8)), dim3(256), 0, st, (const uint16_t*)src, ld, (uint16_t*)dst, rows, K, (int)kp, wide,
+                       targets, ignore);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
-int transpose(const void* src, int64_t ld, void* dst, int64_t ldt, int rows, int K, const int64_t* targets, int64_t ignore, hipStream_t st) {
-    const dim3 grid((unsigned)(up_to(rows, 64) / 64), (unsigned)(up_to(K, 64) / 64));
-    if (grid.y > 65535u) return ROV_ERR_UNSUPPORTED;
-    if (aligned(src, 16) && ld % 8 == 0)
-        hipLaunchKernelGGL((xent_transpose_kernel<true>), grid, dim3(256), 0, st, (const uint16_t*)src, ld, (uint16_t*)dst, ldt, rows, K, targets, ignore);
-    else
-        hipLaunchKernelGGL((xent_transpose_kernel<false>), grid, dim3(256), 0, st, (const uint16_t*)src, ld, (uint16_t*)dst, ldt, rows, K, targets, ignore);
-    ROV_LAUNCH_CHECK();
-    return ROV_OK;
-}
-// out [M][N] = A W^T summed over `shares` of k; sum == NULL (one share): at once, else through sum, to which it is added (`add`), and
-// from there to out if `last`.
-int product(const void* A, int64_t lda, const void* W, int64_t ldw, void* out, int64_t ldo, int M, int N, int64_t K, int shares, float* sum, int64_t lds,
-            bool add, bool last, hipStream_t st) {
+// out [M][N] (rows of ldo) = A W or A^T W summed over `shares` of k; sum == NULL (one share): at once, else through sum, to which it is added
+// (`add`), and from there to out if `last`.  Strides in elements.
+int product(int kind, const void* A, int64_t lda, const void* W, int64_t ldw, void* out, int64_t ldo, int M, int N, int K, int shares, float* sum,
+            int64_t lds, bool add, bool last, hipStream_t st) {
     HeadArgs h;
     h.ld_a = (size_t)lda * 2;
     h.ld_w = (size_t)ldw * 2;
@@ -342,7 +309,7 @@ int product(const void* A, int64_t lda, const void* W, int64_t ldw, void* out, i
     h.add = add;
     h.ld_out = ldo;
     h.out_wide = aligned(out, 8) && ldo % 4 == 0;
-    const int rc = launch_gemm_head(HEAD_SUM, A, W, out, M, N, (int)K, 1.0f, shares, h, st);
+    const int rc = launch_gemm_head(kind, A, W, out, M, N, K, 1.0f, shares, h, st);
     if (rc != ROV_OK || sum == nullptr || !last) return rc;
     hipLaunchKernelGGL(xent_fold_kernel, dim3(sweep_grid((int64_t)M * lds / 4)), dim3(256), 0, st, sum, shares, lds, (uint16_t*)out, ldo, (int64_t)M, N);
     ROV_LAUNCH_CHECK();
@@ -351,10 +318,13 @@ int product(const void* A, int64_t lda, const void* W, int64_t ldw, void* out, i
 bool rows_fit(const void* p, int64_t ld, int K) { return K % 8 == 0 && ld % 8 == 0 && aligned(p, 16); }
 constexpr float kLog2e = 1.44269504088896341f;
 
-int check_head(int M, int V, int K, int64_t ldx, int64_t ldw) {
-    // 256-row panels of every operand are addressed with 32-bit byte offsets, sizes are products' ints
-    const int64_t most = ((int64_t)1 << 32) / 512 - 64;
-    if (K > most || ldx > most || ldw > most || M > most) return ROV_ERR_UNSUPPORTED;
+// Operands are addressed with 32-bit byte offsets: 256 rows, or all rows of k of the products for dX (a piece of W) and dW (X, G).
+int check_head(int M, int K, int64_t ldx, int64_t ldw, const HeadLayout& l, bool backward) {
+    const int64_t most = ((int64_t)1 << 32) - 1024;
+    const int64_t ld = ldx > ldw ? ldx : ldw;
+    if (512 * up_to(ld, 8) > most) return ROV_ERR_UNSUPPORTED;
+    if (backward && (up_to(l.piece, 64) * 2 * up_to(ldw, 8) > most || up_to(M, 64) * 2 * l.kp > most || up_to(M, 64) * 2 * up_to(l.piece, 64) > most))
+        return ROV_ERR_UNSUPPORTED;
     return ROV_OK;
 }
 
@@ -372,7 +342,7 @@ int head_forward(const void* X, const void* W, const int64_t* targets, int M, in
         x = ws + l.x;
         h.ld_a = (size_t)l.kp * 2;
         kx = (int)l.kp;
-        int rc = pack(X, ldx, ws + l.x, M, K, l.kp, st);
+        const int rc = pack(X, ldx, ws + l.x, M, K, l.kp, nullptr, 0, st);
         if (rc != ROV_OK) return rc;
     }
     if (fit_w) {
@@ -381,9 +351,9 @@ int head_forward(const void* X, const void* W, const int64_t* targets, int M, in
         if (rc != ROV_OK) return rc;
     } else {
         h.ld_w = (size_t)l.kp * 2;
-        for (int v0 = 0; v0 < V; v0 += l.piece) {
-            const int cols = V - v0 < l.piece ? V - v0 : l.piece;
-            int rc = pack((const char*)W + (size_t)v0 * ldw * 2, ldw, ws + l.w, cols, K, l.kp, st);
+        for (int v0 = 0; v0 < V; v0 += l.packed) {
+            const int cols = V - v0 < l.packed ? V - v0 : l.packed;
+            int rc = pack((const char*)W + (size_t)v0 * ldw * 2, ldw, ws + l.w, cols, K, l.kp, nullptr, 0, st);
             if (rc != ROV_OK) return rc;
             h.v0 = v0;
             h.part = (float2*)(ws + l.part) + (size_t)(v0 / 128) * M;   // (pieces are whole tiles)
@@ -408,52 +378,40 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
     h.ignore = ignore;
     h.vocab = V;
     h.scale = scale;
-    const void* x = X;
-    h.ld_a = (size_t)ldx * 2;
-    int kx = K, rc = ROV_OK;
+    // X without the ignored rows: what they hold must not reach dW
+    int rc = pack(X, ldx, ws + l.x, M, K, l.kp, targets, ignore, st);
+    if (rc != ROV_OK) return rc;
+    const char* const x = ws + l.x;
+    h.ld_a = (size_t)l.kp * 2;
     const bool fit_w = rows_fit(W, ldw, K);
-    if (!fit_w || !rows_fit(X, ldx, K)) {
-        x = ws + l.x;
-        h.ld_a = (size_t)l.kp * 2;
-        kx = (int)l.kp;
-        rc = pack(X, ldx, ws + l.x, M, K, l.kp, st);
-        if (rc != ROV_OK) return rc;
-    }
-    if (dW != nullptr) {
-        rc = transpose(X, ldx, ws + l.xt, l.mp, M, K, targets, ignore, st);
-        if (rc != ROV_OK) return rc;
-    }
-    float* const sum_x = l.shares_x > 1 || l.piece < V ? (float*)(ws + l.sum_x) : nullptr;
+    const int kx = (int)l.kp, piece = fit_w ? l.piece : l.packed;
+    float* const sum_x = l.shares_x > 1 || piece < V ? (float*)(ws + l.sum_x) : nullptr;
     float* const sum_w = l.shares_w > 1 ? (float*)(ws + l.sum_w) : nullptr;
-    for (int v0 = 0; v0 < V; v0 += l.piece) {
-        const int cols = V - v0 < l.piece ? V - v0 : l.piece;
-        const int64_t cp = up_to(cols, 64);
-        const char* const w = (const char*)W + (size_t)v0 * ldw * 2;
-        const void* wk = w;
-        h.ld_w = (size_t)ldw * 2;
+    for (int v0 = 0; v0 < V; v0 += piece) {
+        const int cols = V - v0 < piece ? V - v0 : piece;
+        const int64_t ldg = up_to(cols, 64);
+        const char* w = (const char*)W + (size_t)v0 * ldw * 2;
+        int64_t ld = ldw;
         if (!fit_w) {
-            rc = pack(w, ldw, ws + l.w, cols, K, l.kp, st);
+            rc = pack(w, ldw, ws + l.w, cols, K, l.kp, nullptr, 0, st);
             if (rc != ROV_OK) return rc;
-            wk = ws + l.w;
-            h.ld_w = (size_t)l.kp * 2;
+            w = ws + l.w;
+            ld = l.kp;
         }
+        h.ld_w = (size_t)ld * 2;
         h.v0 = v0;
-        h.g = dX != nullptr ? (uint16_t*)(ws + l.g) : nullptr;
-        h.gt = dW != nullptr ? (uint16_t*)(ws + l.gt) : nullptr;
-        h.ld_g = cp;
-        h.ld_gt = l.mp;
-        rc = launch_gemm_head(HEAD_GRAD, x, wk, nullptr, M, cols, kx, scale * kLog2e, 1, h, st);
+        h.g = (uint16_t*)(ws + l.g);
+        h.ld_g = ldg;
+        rc = launch_gemm_head(HEAD_GRAD, x, w, nullptr, M, cols, kx, scale * kLog2e, 1, h, st);
         if (rc != ROV_OK) return rc;
         if (dX != nullptr) {
-            rc = transpose(w, ldw, ws + l.w, cp, cols, K, nullptr, 0, st);
-            if (rc != ROV_OK) return rc;
             // (the last, shorter piece may have fewer slots of k than shares: the sums of the shares left out stay)
-            const int shares = l.shares_x > cp / 64 ? (int)(cp / 64) : l.shares_x;
-            rc = product(ws + l.g, cp, ws + l.w, cp, dX, lddx, M, K, cp, shares, sum_x, l.ks, v0 > 0, false, st);
+            const int shares = l.shares_x > ldg / 64 ? (int)(ldg / 64) : l.shares_x;
+            rc = product(HEAD_DX, ws + l.g, ldg, w, ld, dX, lddx, M, K, cols, shares, sum_x, l.ks, v0 > 0, false, st);
             if (rc != ROV_OK) return rc;
         }
         if (dW != nullptr) {
-            rc = product(ws + l.gt, l.mp, ws + l.xt, l.mp, (char*)dW + (size_t)v0 * lddw * 2, lddw, cols, K, l.mp, l.shares_w, sum_w, l.ks, false, true, st);
+            rc = product(HEAD_DW, ws + l.g, ldg, x, l.kp, (char*)dW + (size_t)v0 * lddw * 2, lddw, cols, K, M, l.shares_w, sum_w, l.ks, false, true, st);
             if (rc != ROV_OK) return rc;
         }
     }
@@ -496,8 +454,8 @@ extern "C" int rov_linear_xent(const void* X, const void* W, const int64_t* targ
     if (loss == nullptr || lse == nullptr || !aligned(loss, 4) || !aligned(lse, 4)) return ROV_ERR_INVALID;
     if (workspace == nullptr || !aligned(workspace, kAlign)) return ROV_ERR_INVALID;
     if (dtype == ROV_BF16) {
-        ROV_STEP(check_head(M, V, K, ldx, ldw));
         const HeadLayout hl = head_layout(M, V, K, vocab_piece, false);
+        ROV_STEP(check_head(M, K, ldx, ldw, hl, false));
         if (workspace_bytes < hl.total) return ROV_ERR_WORKSPACE;
         return head_forward(X, W, targets, M, V, K, ldx, ldw, scale, ignore_index, loss, lse, (char*)workspace, hl, (hipStream_t)stream);
     }
@@ -536,8 +494,8 @@ extern "C" int rov_linear_xent_bwd(const void* X, const void* W, const int64_t* 
     if ((dX != nullptr && (lddx < K || !aligned(dX, esz))) || (dW != nullptr && (lddw < K || !aligned(dW, esz)))) return ROV_ERR_INVALID;
     if (workspace == nullptr || !aligned(workspace, kAlign)) return ROV_ERR_INVALID;
     if (dtype == ROV_BF16) {
-        ROV_STEP(check_head(M, V, K, ldx, ldw));
         const HeadLayout hl = head_layout(M, V, K, vocab_piece, true);
+        ROV_STEP(check_head(M, K, ldx, ldw, hl, true));
         if (workspace_bytes < hl.total) return ROV_ERR_WORKSPACE;
         return head_backward(X, W, targets, lse, dloss, dlse, M, V, K, ldx, ldw, scale, ignore_index, dX, dW, lddx, lddw, (char*)workspace, hl,
                              (hipStream_t)stream);
