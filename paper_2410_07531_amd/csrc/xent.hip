@@ -136,13 +136,15 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restri
     }
 }
 
-// Joins the statistics part[count][M] of M rows (units of log 2) and writes the results: 16 rows a workgroup, 16 threads a row.
+// Joins the statistics part[count][M] of M rows (units of log 2) and writes the results: R rows a workgroup, 256 / R threads a row.
+template <int R>
 __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict__ part, int count, const float* __restrict__ picked, int M, int V,
                                                         const int64_t* __restrict__ targets, int64_t ignore, float* __restrict__ loss,
                                                         float* __restrict__ lse) {
-    __shared__ float2 red[16][16];
-    const int r = threadIdx.x & 15, slice = threadIdx.x >> 4;
-    const int64_t m = (int64_t)blockIdx.x * 16 + r;
+    constexpr int SLICES = 256 / R;
+    __shared__ float2 red[SLICES][R];
+    const int r = threadIdx.x % R, slice = threadIdx.x / R;
+    const int64_t m = (int64_t)blockIdx.x * R + r;
     float top = -INFINITY, sum = 0.0f;
     auto join = [&](float2 v) {
         const float t = fmaxf(top, v.x), base = t > -INFINITY ? t : 0.0f;
@@ -150,12 +152,17 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
         top = t;
     };
     if (m < M)
-#pragma unroll 4
-        for (int c = slice; c < count; c += 16) join(part[(int64_t)c * M + m]);
+#pragma unroll 8
+        for (int c = slice; c < count; c += SLICES) join(part[(int64_t)c * M + m]);
     red[slice][r] = make_float2(top, sum);
     __syncthreads();
+    if (slice < 8) {
+        for (int i = slice + 8; i < SLICES; i += 8) join(red[i][r]);
+        red[slice][r] = make_float2(top, sum);
+    }
+    __syncthreads();
     if (slice != 0 || m >= M) return;
-    for (int i = 1; i < 16; ++i) join(red[i][r]);
+    for (int i = 1; i < 8; ++i) join(red[i][r]);
     constexpr double ln2 = 0.69314718055994530942;
     const float base = top > -INFINITY ? top : 0.0f;
     // (units of log 2 -> of e in double: the loss is a difference of two such values)
@@ -163,6 +170,115 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
     const int64_t t = targets[m];
     lse[m] = (float)l;
     loss[m] = t == ignore ? 0.0f : in_vocab(t, V) ? (float)(l - (double)picked[m] * ln2) : NAN;
+}
+
+// dW [V][K] (rows of ldo) = G^T X over at most 64 * SLOTS rows: G [M][ldg], X [M][ldx], both with rows of whole 16-byte chunks.
+// What bounds it: dW's bytes.  A 256 x 256 tile of gemm.hip has one or two slots of 64 rows to walk here, and with one workgroup a compute unit
+// nothing runs while its operands travel and its results leave.  Here a workgroup keeps 128 columns of X in registers, walks over
+// tiles of 128 columns of G, the next of which is on its way, and three (two) workgroups share a compute unit.  131072 x 4096, us, 256 x 256
+// tiles / this: 16 rows 425 / 259 (4.1 TB/s), 64 rows 462 / 288, 128 rows 515 / 360.
+// Four waves, 64 x 64 each; tiles lie in LDS as 64 rows of 128 columns (256 bytes, the chunk swizzle of gemm_ring.hip's [K, N] tiles), fragments
+// come by the transposing LDS load; X's columns are dealt so that a lane ends up with eight neighbours and stores 16 bytes.
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4* lds_i16x4_ptr;
+
+template <int SLOTS>
+__global__ __launch_bounds__(256, SLOTS == 1 ? 3 : 2) void xent_outer_kernel(const uint16_t* __restrict__ G, int64_t ldg, const uint16_t* __restrict__ X, int64_t ldx,
+                                                           uint16_t* __restrict__ out, int64_t ldo, bool out_wide, int V, int K, int M, int tiles_v) {
+    constexpr int kTile = SLOTS * 64 * 256;
+    __shared__ __attribute__((aligned(16))) char lds[2][kTile];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wv = wave >> 1, wk = wave & 1;
+    const int k0 = blockIdx.x * 128;
+    auto swz = [](int row) { return ((row & 3) | (((row >> 3) & 1) << 2)) << 1; };
+    // thread t moves chunk t % 16 of rows t / 16 + 16 * i
+    const int chunk = threadIdx.x & 15, row0 = threadIdx.x >> 4;
+    uint4 next[4 * SLOTS];
+    auto fetch = [&](const uint16_t* from, int64_t ld, int col) {
+        const bool in = col + chunk * 8 < ld;
+#pragma unroll
+        for (int i = 0; i < 4 * SLOTS; ++i) {
+            const int m = row0 + 16 * i;
+            next[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (m < M && in) next[i] = *reinterpret_cast<const uint4*>(from + (int64_t)m * ld + col + chunk * 8);
+        }
+    };
+    auto put = [&](char* to) {
+#pragma unroll
+        for (int i = 0; i < 4 * SLOTS; ++i) {
+            const int row = row0 + 16 * i;
+            *reinterpret_cast<uint4*>(to + row * 256 + ((chunk ^ swz(row)) << 4)) = next[i];
+        }
+    };
+    // lane 16q + 4r + s supplies rows 32h + 8q (+4) + r, four columns of a block, and receives its own column's values
+    const int r = (lane >> 2) & 3, q = lane >> 4, s = lane & 3, f = (r | ((q & 1) << 2)) << 1;
+    auto fragment = [&](const char* from, int h, int byte) {
+        char* const at = const_cast<char*>(from) + (32 * h + 8 * q + r) * 256 + ((((byte >> 4) ^ f) << 4) | (byte & 8));
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)at);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + 4 * 256));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    fetch(X, ldx, k0);
+    put(lds[1]);
+    int tile = blockIdx.y;   // (the grid has no more rows than tiles)
+    fetch(G, ldg, tile * 128);
+    __syncthreads();
+    // block j holds columns 32 * (j / 2) + 8 * (c / 4) + 4 * (j % 2) + c % 4, c = 0 .. 15
+    bf16x8 b[2 * SLOTS][4];
+#pragma unroll
+    for (int h = 0; h < 2 * SLOTS; ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[h][j] = fragment(lds[1], h, wk * 128 + (j >> 1) * 64 + s * 16 + (j & 1) * 8);
+    put(lds[0]);
+    __syncthreads();
+    const int steps = (M + 31) / 32;
+    for (int buf = 0; tile < tiles_v; buf ^= 1) {
+        const int here = tile;
+        tile += gridDim.y;
+        if (tile < tiles_v) fetch(G, ldg, tile * 128);
+        f32x4 acc[4][4];   // [16 columns of X][16 columns of G]
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][i][e] = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2 * SLOTS; ++h) {
+            if (h >= steps) break;
+            bf16x8 a[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = fragment(lds[buf], h, wv * 128 + i * 32 + s * 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[h][j], a[i], acc[j][i], 0, 0, 0);
+        }
+        if (tile < tiles_v) put(lds[buf ^ 1]);   // (last read two tiles ago, a barrier between)
+        // a lane holds column lane % 16 of G's block and eight columns of X's two blocks
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int v = here * 128 + wv * 64 + i * 16 + (lane & 15);
+            if (v >= V) continue;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int k = k0 + wk * 64 + t * 32 + q * 8;
+                uint16_t* const to = out + (int64_t)v * ldo + k;
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = bf16_pair(acc[2 * t + (e >> 1)][i][2 * (e & 1)], acc[2 * t + (e >> 1)][i][2 * (e & 1) + 1]);
+                if (out_wide && k + 7 < K) {
+                    *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (k + e < K) to[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                }
+            }
+        }
+        __syncthreads();
+    }
 }
 
 // out [rows][K] (bf16, rows of ldo) = sum over shares of sums[share][rows][lds].
@@ -173,6 +289,7 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const float* __restrict_
         const int64_t r = i / quads;
         const int c = (int)(i - r * quads) * 4;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
         for (int k = 0; k < shares; ++k) {
             const float4 v = *reinterpret_cast<const float4*>(sums + ((int64_t)k * rows + r) * lds + c);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -315,6 +432,20 @@ int product(int kind, const void* A, int64_t lda, const void* W, int64_t ldw, vo
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
+int outer(const void* G, int64_t ldg, const void* X, int64_t ldx, uint16_t* out, int64_t ldo, int V, int K, int M, hipStream_t st) {
+    const int64_t tiles_k = up_to(K, 128) / 128, tiles_v = up_to(V, 128) / 128;
+    int64_t rows = 3 * device_cu_count() / tiles_k;   // as many workgroups as run at once
+    if (rows > tiles_v) rows = tiles_v;
+    if (rows < 1) rows = 1;
+    const bool wide = aligned(out, 16) && ldo % 8 == 0;
+    const dim3 grid((unsigned)tiles_k, (unsigned)rows);
+    if (M <= 64)
+        hipLaunchKernelGGL(xent_outer_kernel<1>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v);
+    else
+        hipLaunchKernelGGL(xent_outer_kernel<2>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v);
+    ROV_LAUNCH_CHECK();
+    return ROV_OK;
+}
 bool rows_fit(const void* p, int64_t ld, int K) { return K % 8 == 0 && ld % 8 == 0 && aligned(p, 16); }
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -361,8 +492,13 @@ int head_forward(const void* X, const void* W, const int64_t* targets, int M, in
             if (rc != ROV_OK) return rc;
         }
     }
-    hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((M + 15) / 16)), dim3(256), 0, st, (const float2*)(ws + l.part), 2 * gemm_head_tiles_n(V),
-                       h.picked, M, V, targets, ignore, loss, lse);
+    // (few rows: more threads a row, 16 x 131072 12 -> 5 us)
+    if (M < 1024)
+        hipLaunchKernelGGL(xent_join_kernel<4>, dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, (const float2*)(ws + l.part), 2 * gemm_head_tiles_n(V),
+                           h.picked, M, V, targets, ignore, loss, lse);
+    else
+        hipLaunchKernelGGL(xent_join_kernel<16>, dim3((unsigned)((M + 15) / 16)), dim3(256), 0, st, (const float2*)(ws + l.part),
+                           2 * gemm_head_tiles_n(V), h.picked, M, V, targets, ignore, loss, lse);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
@@ -411,6 +547,11 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
             if (rc != ROV_OK) return rc;
         }
         if (dW != nullptr) {
+            if (M <= 128) {
+                rc = outer(ws + l.g, ldg, x, l.kp, (uint16_t*)dW + (size_t)v0 * lddw, lddw, cols, K, M, st);
+                if (rc != ROV_OK) return rc;
+                continue;
+            }
             rc = product(HEAD_DW, ws + l.g, ldg, x, l.kp, (char*)dW + (size_t)v0 * lddw * 2, lddw, cols, K, M, l.shares_w, sum_w, l.ks, false, true, st);
             if (rc != ROV_OK) return rc;
         }
