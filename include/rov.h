@@ -597,6 +597,31 @@ int rov_norm_residual_bwd(const void *y, const void *h, const void *w_post, cons
                           float x_scale, float h_scale, float eps, void *workspace, size_t workspace_bytes,
                           void *stream);
 
+/* rov_block_forward with these two operators inside, for blocks of other shapes:
+ *   rope                     turns q and k (NULL: the block's own form, rope_theta), by `positions` as in rov_rope
+ *   post1, gate1, post2, gate2, x_scale, h_scale   the residual sums behind attention's projection and behind the feed-forward become
+ *                            x2 = x_scale * x + h_scale * gate1 * P(a Wo^T), P(h) = RMS(h) * post1 (h itself without post1), and
+ *                            y = x_scale * x2 + h_scale * gate2 * P(u Wd^T) with post2;
+ *                            post1, post2 [hidden], gates [B*S / rows_per_gate, hidden] (rows_per_gate 0: one for all), bf16,
+ *                            each may be NULL; scales of 1 with all four NULL: the plain residual.  The branch is rounded to bf16 before P.
+ * Everything else, the workspace's size and errors included, as in rov_block_forward.  opts lies in host memory. */
+typedef struct rov_block_opts {
+    const rov_rope_cfg *rope;
+    const int64_t *positions;
+    int64_t positions_stride;
+    const void *post1;
+    const void *gate1;
+    const void *post2;
+    const void *gate2;
+    int64_t rows_per_gate;
+    float x_scale, h_scale;
+} rov_block_opts;
+
+int rov_block_forward_opts(const rov_block_weights *w, const rov_block_opts *opts, const void *x, void *y, int B, int S,
+                           const rov_block_cfg *cfg, int schedule, uint64_t seed, uint64_t offset, int mask_ready,
+                           uint64_t *mask, uint64_t *next_mask, void *workspace, size_t workspace_bytes,
+                           void *main_stream, void *side_stream);
+
 /* ---------------------------------------------------------------- loss over the vocabulary
  * Softmax cross entropy of the logits z = scale * X W^T, X [M, K] hidden states, W [V, K] output weights, without
  * keeping z (M x V): the vocabulary is walked in pieces.

@@ -62,6 +62,12 @@ class RopeCfg(ctypes.Structure):
                 ("turns_high", ctypes.c_float), ("magnitude", ctypes.c_float)]
 
 
+class BlockOpts(ctypes.Structure):
+    _fields_ = [("rope", ctypes.POINTER(RopeCfg)), ("positions", ctypes.c_void_p), ("positions_stride", ctypes.c_int64),
+                ("post1", ctypes.c_void_p), ("gate1", ctypes.c_void_p), ("post2", ctypes.c_void_p), ("gate2", ctypes.c_void_p),
+                ("rows_per_gate", ctypes.c_int64), ("x_scale", ctypes.c_float), ("h_scale", ctypes.c_float)]
+
+
 # name -> (restype, argtypes); also the list of symbols the header declares
 _u64, _i, _f, _p = ctypes.c_uint64, ctypes.c_int, ctypes.c_float, ctypes.c_void_p
 _i64 = ctypes.c_int64
@@ -118,6 +124,8 @@ SIGNATURES = {
     "rov_set_block_hybrid_mask_rows": (_i, [_i]),
     "rov_block_forward": (_i, [ctypes.POINTER(BlockWeights), _p, _p, _i, _i, ctypes.POINTER(BlockCfg),
                                _i, _u64, _u64, _i, _p, _p, _p, ctypes.c_size_t, _p, _p]),
+    "rov_block_forward_opts": (_i, [ctypes.POINTER(BlockWeights), ctypes.POINTER(BlockOpts), _p, _p, _i, _i, ctypes.POINTER(BlockCfg),
+                                    _i, _u64, _u64, _i, _p, _p, _p, ctypes.c_size_t, _p, _p]),
     "rov_mask_finish": (_i, [_p, _p]),
     "rov_block_static_scratch_bytes": (ctypes.c_size_t, []),
     "rov_block_forward_static": (_i, [ctypes.POINTER(BlockWeights), _p, _p, _i, _i, ctypes.POINTER(BlockCfg),
@@ -523,16 +531,27 @@ def make_block_weights(w, w_scale=None):
     return BlockWeights(*[w[n].data_ptr() for n in ("norm1", "norm2") + names], sc)
 
 
+def make_block_opts(rope=None, positions=None, post1=None, gate1=None, post2=None, gate2=None, rows_per_gate=0, x_scale=1.0, h_scale=1.0):
+    """Rotary form (make_rope_cfg; positions int64 [B, S] or [S]), post norms, gates and residual scales of a block (rov_block_opts).
+    The caller keeps the tensors; the opts keep the rotary form."""
+    ptr = lambda t: t.data_ptr() if t is not None else None
+    stride = positions.stride(0) if positions is not None and positions.dim() == 2 and positions.shape[0] > 1 else 0
+    return BlockOpts(ctypes.pointer(rope) if rope is not None else None, ptr(positions), stride, ptr(post1), ptr(gate1), ptr(post2), ptr(gate2),
+                     int(rows_per_gate), float(x_scale), float(h_scale))
+
+
 def block_forward(weights, x, y, cfg, schedule, seed, offset, mask, workspace, main_stream, side_stream,
-                  mask_ready=False, next_mask=None):
+                  mask_ready=False, next_mask=None, opts=None):
+    """opts: make_block_opts, for blocks with other rotary forms, post norms, gates or residual scales."""
     B, S, _ = x.shape
     mptr = mask.data_ptr() if mask is not None else None
     nptr = next_mask.data_ptr() if next_mask is not None else None
-    _check(load().rov_block_forward(ctypes.byref(weights), x.data_ptr(),
-                                    y.data_ptr(), B, S, ctypes.byref(cfg), int(schedule),
-                                    seed & (2**64 - 1), offset & (2**64 - 1), int(mask_ready), mptr, nptr,
-                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                    _stream_ptr(main_stream), _stream_ptr(side_stream)), "rov_block_forward")
+    rest = (x.data_ptr(), y.data_ptr(), B, S, ctypes.byref(cfg), int(schedule), seed & (2**64 - 1), offset & (2**64 - 1), int(mask_ready),
+            mptr, nptr, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(main_stream), _stream_ptr(side_stream))
+    if opts is not None:
+        _check(load().rov_block_forward_opts(ctypes.byref(weights), ctypes.byref(opts), *rest), "rov_block_forward_opts")
+    else:
+        _check(load().rov_block_forward(ctypes.byref(weights), *rest), "rov_block_forward")
     return y
 
 

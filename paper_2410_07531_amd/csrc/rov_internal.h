@@ -161,6 +161,18 @@ int launch_rmsnorm(const void* x, const void* weight, void* y, int64_t rows, int
 // y8 (bytes, [rows, n]) = e4m3(RMSNorm(x) * weight / scale): the fp8 block's quantised activations.
 int launch_rmsnorm_fp8(const void* x, const void* weight, void* y8, int64_t rows, int n, float eps, float scale,
                        hipStream_t stream);
+// rope.hip, norm.hip: see rov_rope and rov_norm_residual
+int check_rope(const rov_rope_cfg* c, const void* Q, const void* Qo, const void* K, const void* Ko, int B, int S, int H, int Hkv, int d,
+               const int64_t strides[12], int dtype);
+int launch_rope_cfg(const rov_rope_cfg* c, const void* Q, void* Qo, const void* K, void* Ko, int B, int S, int H, int Hkv, int d,
+                    const int64_t strides[12], int dtype, const int64_t* positions, int64_t positions_stride, int backward, hipStream_t stream);
+int check_norm_residual(const void* x, const void* h, const void* w_post, const void* gate, const void* w_pre, const void* y, const void* yn,
+                        int64_t rows, int n, const int64_t ld[4], int64_t rows_per_gate, int dtype, float x_scale, float h_scale, float eps,
+                        float yn_fp8_scale);
+int launch_norm_residual(const void* x, const void* h, const void* w_post, const void* gate, const void* w_pre, void* y, void* yn, int64_t rows, int n,
+                         const int64_t ld[4], int64_t rows_per_gate, int dtype, float x_scale, float h_scale, float eps, float yn_fp8_scale,
+                         hipStream_t stream);
+
 int launch_rope(void* buf, int64_t tokens, int64_t row_elems, int S, int nheads, int d, float theta,
                 hipStream_t stream);
 

@@ -564,7 +564,7 @@ extern "C" int rov_set_block_hybrid_mask_rows(int rows) { return rov::g_hybrid_r
 
 namespace rov {
 namespace {
-int block_forward_impl(const rov_block_weights* w, const void* x, void* y, int B, int S,
+int block_forward_impl(const rov_block_weights* w, const rov_block_opts* opts, const void* x, void* y, int B, int S,
                        const rov_block_cfg* cfg, int schedule, uint64_t seed,
                        uint64_t offset, int mask_ready, uint64_t* mask,
                        uint64_t* next_mask, void* workspace, size_t workspace_bytes,
@@ -634,10 +634,19 @@ int block_forward_impl(const rov_block_weights* w, const void* x, void* y, int B
         (int64_t)S * qkv_n, qkv_n, d,      // K
         (int64_t)S * qkv_n, qkv_n, d,      // V
         (int64_t)S * H * d, (int64_t)H * d, d};   // O (elements: bf16, or bytes when fp8)
+    const int64_t rope_strides[12] = {(int64_t)S * qkv_n, qkv_n, d, (int64_t)S * qkv_n, qkv_n, d,
+                                      (int64_t)S * qkv_n, qkv_n, d, (int64_t)S * qkv_n, qkv_n, d};
     // fp8: the attention output is quantised in the attention kernel's epilogue and lives, as bytes, in
     // the slot of the SwiGLU output (free until FC1 runs, after the PROJ GEMM has consumed it)
     void* att_out = f8 ? u : att;
     const float att_q = f8 ? sa1 : 0.0f;
+    // other forms of residual: the projections leave their products alone, in the place of the sum, and the norm kernel makes the sum of
+    // it there, together with the norm that follows
+    const rov_rope_cfg* const rope = opts != nullptr ? opts->rope : nullptr;
+    const bool around = opts != nullptr && (opts->post1 != nullptr || opts->post2 != nullptr || opts->gate1 != nullptr || opts->gate2 != nullptr ||
+                                            opts->x_scale != 1.0f || opts->h_scale != 1.0f);
+    const int64_t per_gate = around && opts->rows_per_gate != 0 ? opts->rows_per_gate : T;
+    const int64_t lds[4] = {hidden, hidden, hidden, hidden};
     int rc = ROV_OK;
     // every kernel of the block is checked before the first one is enqueued
 #define ROV_STEP(expr)            \
@@ -647,12 +656,20 @@ int block_forward_impl(const rov_block_weights* w, const void* x, void* y, int B
     } while (0)
     if ((hidden % 8) != 0 || (d % 8) != 0) return ROV_ERR_UNSUPPORTED;   // RMSNorm / RoPE vector width
     ROV_STEP(check_gemm(h, w->wqkv, qkv, nullptr, EPI_ADD, (int)T, qkv_n, hidden, dt, 1));
-    ROV_STEP(check_gemm(att_out, w->wo, x2, x, EPI_ADD, (int)T, hidden, H * d, dt, 1));
+    ROV_STEP(check_gemm(att_out, w->wo, x2, around ? nullptr : x, EPI_ADD, (int)T, hidden, H * d, dt, 1));
     if (f8)
         ROV_STEP(check_gemm_swiglu_fp8(h, w->wg, w->wu, u, (int)T, ffn, hidden, sa3));
     else
         ROV_STEP(check_gemm_swiglu(h, w->wg, w->wu, u, (int)T, ffn, hidden));
-    ROV_STEP(check_gemm(u, w->wd, y, x2, EPI_ADD, (int)T, hidden, ffn, dt, 1));
+    ROV_STEP(check_gemm(u, w->wd, y, around ? nullptr : x2, EPI_ADD, (int)T, hidden, ffn, dt, 1));
+    if (rope != nullptr)
+        ROV_STEP(check_rope(rope, qkv, qkv, (char*)qkv + (size_t)H * d * 2, (char*)qkv + (size_t)H * d * 2, B, S, H, Hkv, d, rope_strides, ROV_BF16));
+    if (around) {
+        ROV_STEP(check_norm_residual(x, x2, opts->post1, opts->gate1, w->norm2, x2, h, T, hidden, lds, per_gate, ROV_BF16, opts->x_scale, opts->h_scale,
+                                     cfg->eps, f8 ? sa2 : 0.0f));
+        ROV_STEP(check_norm_residual(x2, y, opts->post2, opts->gate2, nullptr, y, nullptr, T, hidden, lds, per_gate, ROV_BF16, opts->x_scale,
+                                     opts->h_scale, cfg->eps, 0.0f));
+    }
     ROV_STEP(check_attention_rows(qp, qp + (int64_t)H * d, qp + (int64_t)(H + Hkv) * d, att_out, B, H, Hkv, S, d, strides,
                                   ROV_BF16, cfg->p, use_mask ? mask : nullptr, 0, S, 10, 32));
     if (use_mask) ROV_STEP(check_mask(B, H, S, cfg->p, 10, 32, mask));
@@ -726,6 +743,10 @@ int block_forward_impl(const rov_block_weights* w, const void* x, void* y, int B
         // block's QKV GEMM (paper Sec. 3.3)
         ROV_STEP(t_mask(seed, offset, B, H, S, cfg->p, mask, ms, MASK_GRID_HELPER, fl.split, cfg->causal != 0));
     ROV_STEP(traced(ROV_TRACE_GLUE, ms, [&] {   // q heads then k heads
+        if (rope != nullptr) {
+            void* const k = (char*)qkv + (size_t)H * d * 2;
+            return launch_rope_cfg(rope, qkv, qkv, k, k, B, S, H, Hkv, d, rope_strides, ROV_BF16, opts->positions, opts->positions_stride, 0, ms);
+        }
         return launch_rope(qkv, T, qkv_n, S, H + Hkv, d, cfg->rope_theta, ms);
     }));
     if (use_mask && !mask_ready && overlap) {
@@ -771,7 +792,7 @@ int block_forward_impl(const rov_block_weights* w, const void* x, void* y, int B
         if (R == S) ROV_STEP(plan_split(rest + (defer ? qkv_flop : 0.0), dt, mask_calls, B, H, S, ms, &next));
         ROV_STEP(side.fork());
     }
-    ROV_STEP(t_gemm(att_out, w->wo, x2, x, (int)T, hidden, H * d, dt, 1, sa1, sw_o, ms));
+    ROV_STEP(t_gemm(att_out, w->wo, x2, around ? nullptr : x, (int)T, hidden, H * d, dt, 1, sa1, sw_o, ms));
     if (run_ahead) {
         if (R < S)
             ROV_STEP(traced(ROV_TRACE_RNG, ss, [&] {
@@ -784,6 +805,9 @@ int block_forward_impl(const rov_block_weights* w, const void* x, void* y, int B
         ROV_STEP(side.mark());
     }
     ROV_STEP(traced(ROV_TRACE_GLUE, ms, [&] {
+        if (around)
+            return launch_norm_residual(x, x2, opts->post1, opts->gate1, w->norm2, x2, h, T, hidden, lds, per_gate, ROV_BF16, opts->x_scale,
+                                        opts->h_scale, cfg->eps, f8 ? sa2 : 0.0f, ms);
         return f8 ? launch_rmsnorm_fp8(x2, w->norm2, h, T, hidden, cfg->eps, sa2, ms)
                   : launch_rmsnorm(x2, w->norm2, h, T, hidden, cfg->eps, ms);
     }));
@@ -793,7 +817,12 @@ int block_forward_impl(const rov_block_weights* w, const void* x, void* y, int B
         return f8 ? launch_gemm_swiglu_fp8(h, w->wg, w->wu, u, (int)T, ffn, hidden, sa2, sw_g, sw_u, sa3, ms)
                   : launch_gemm_swiglu(h, w->wg, w->wu, u, (int)T, ffn, hidden, ms);
     }));
-    ROV_STEP(t_gemm(u, w->wd, y, x2, (int)T, hidden, ffn, dt, 1, sa3, sw_d, ms));
+    ROV_STEP(t_gemm(u, w->wd, y, around ? nullptr : x2, (int)T, hidden, ffn, dt, 1, sa3, sw_d, ms));
+    if (around)
+        ROV_STEP(traced(ROV_TRACE_GLUE, ms, [&] {
+            return launch_norm_residual(x2, y, opts->post2, opts->gate2, nullptr, y, nullptr, T, hidden, lds, per_gate, ROV_BF16, opts->x_scale,
+                                        opts->h_scale, cfg->eps, 0.0f, ms);
+        }));
     if (run_ahead && defer && R == S) {
         // left in flight: the following block (mask_ready == ROV_MASK_IN_FLIGHT) helps and joins
         g_in_flight[next_mask] = InFlightMask{ss, next, seed, offset + rov_mask_philox_calls(B, H, S), B, H, S,
@@ -875,7 +904,16 @@ extern "C" int rov_block_forward(const rov_block_weights* w, const void* x, void
                                  uint64_t offset, int mask_ready, uint64_t* mask,
                                  uint64_t* next_mask, void* workspace, size_t workspace_bytes,
                                  void* main_stream, void* side_stream) {
-    return rov::block_forward_impl(w, x, y, B, S, cfg, schedule, seed, offset, mask_ready, mask, next_mask, workspace,
+    return rov::block_forward_impl(w, nullptr, x, y, B, S, cfg, schedule, seed, offset, mask_ready, mask, next_mask, workspace,
+                                   workspace_bytes, main_stream, side_stream);
+}
+
+extern "C" int rov_block_forward_opts(const rov_block_weights* w, const rov_block_opts* opts, const void* x, void* y, int B, int S,
+                                      const rov_block_cfg* cfg, int schedule, uint64_t seed, uint64_t offset, int mask_ready,
+                                      uint64_t* mask, uint64_t* next_mask, void* workspace, size_t workspace_bytes, void* main_stream,
+                                      void* side_stream) {
+    if (opts == nullptr) return ROV_ERR_INVALID;
+    return rov::block_forward_impl(w, opts, x, y, B, S, cfg, schedule, seed, offset, mask_ready, mask, next_mask, workspace,
                                    workspace_bytes, main_stream, side_stream);
 }
 
@@ -895,6 +933,6 @@ extern "C" int rov_block_forward_static(const rov_block_weights* w, const void* 
     void* ws = nullptr;
     const int rc = rov::static_scratch_ptr(&ws);
     if (rc != ROV_OK) return rc;
-    return rov::block_forward_impl(w, x, y, B, S, cfg, schedule, seed, offset, mask_ready, mask, next_mask, ws,
+    return rov::block_forward_impl(w, nullptr, x, y, B, S, cfg, schedule, seed, offset, mask_ready, mask, next_mask, ws,
                                    rov::kStaticScratchBytes, main_stream, side_stream);
 }

@@ -1,0 +1,179 @@
+"""The operators around the block as a program uses them together: a block with its own rotary form, post norms, gates and
+residual scales, the loss behind it, and the gradients back through loss, norms and rotary positions.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import dense as OD
+from oracle import philox as OP
+from paper_2410_07531_amd import binding as rov
+from paper_2410_07531_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+DIMS = dict(H=4, Hkv=2, d=128, hidden=512, ffn=1088)
+ROPE = dict(rot=96, theta=10000.0, layout=rov.ROPE_HALVES, scaling=rov.ROPE_SCALE_PARTS, factor=4.0, turns_low=1.0, turns_high=8.0, trained_len=256,
+            magnitude=1.1)
+
+
+def _f64(t):
+    return t.double().cpu().numpy()
+
+
+def _setup(B, S, seed):
+    rng = np.random.default_rng(seed)
+    to = lambda a: torch.from_numpy(a).to(torch.bfloat16).cuda()
+    w = {k: to(v) for k, v in wl.block_weights(rng, *(DIMS[k] for k in ("H", "Hkv", "d", "hidden", "ffn"))).items()}
+    x = to(wl.block_input(rng, B, S, DIMS["hidden"]))
+    around = {k: to((1.0 + 0.1 * rng.standard_normal(DIMS["hidden"])).astype(np.float32)) for k in ("post1", "post2")}
+    around.update({k: to((0.5 + 0.3 * rng.standard_normal((B, DIMS["hidden"]))).astype(np.float32)) for k in ("gate1", "gate2")})
+    return x, w, around, torch.from_numpy(rng.integers(0, 3000, (B, 1)) + np.arange(S)).cuda()
+
+
+def _rope(x, pos):
+    import test_gpu_rope as R
+    return R.reference(torch.from_numpy(x), torch.from_numpy(pos), ROPE)[0].numpy()
+
+
+def _reference(x, w, around, pos, keep, p, causal, x_scale, h_scale):
+    B, S, hidden = x.shape
+    H, Hkv, d = DIMS["H"], DIMS["Hkv"], DIMS["d"]
+    qkv = OD.rmsnorm(x, w["norm1"], 1e-5) @ w["wqkv"].T
+    q, k, v = (qkv[..., a * d:b * d].reshape(B, S, b - a, d) for a, b in ((0, H), (H, H + Hkv), (H + Hkv, H + 2 * Hkv)))
+    a = OD.attention_dropout(_rope(q, pos), _rope(k, pos), v, keep, p, causal=causal).reshape(B, S, H * d)
+    x2 = x_scale * x + h_scale * around["gate1"][:, None] * OD.rmsnorm(a @ w["wo"].T, around["post1"], 1e-5)
+    h2 = OD.rmsnorm(x2, w["norm2"], 1e-5)
+    u = OD.silu(h2 @ w["wg"].T) * (h2 @ w["wu"].T)
+    return x_scale * x2 + h_scale * around["gate2"][:, None] * OD.rmsnorm(u @ w["wd"].T, around["post2"], 1e-5)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_block_with_other_forms_matches_the_definition(causal):
+    # bf16 tensors between kernels: the tolerance of the plain block against the oracle (2e-2 of the largest value); the three
+    # schedules drop the same elements and agree bit for bit
+    B, S, p, seed, offset = 2, 160, 0.1, wl.SEED, 320
+    x, w, around, pos = _setup(B, S, 71)
+    cfg = rov.make_block_cfg(*(DIMS[k] for k in ("H", "Hkv", "d", "hidden", "ffn")), p, causal=causal)
+    ws = torch.empty(rov.block_workspace_bytes(cfg, B, S, 0), dtype=torch.uint8, device="cuda")
+    form = rov.make_rope_cfg(**ROPE)
+    opts = rov.make_block_opts(rope=form, positions=pos, rows_per_gate=S, x_scale=0.9, h_scale=0.5, **around)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    ys = []
+    for sched in (rov.SCHED_SEQUENTIAL, rov.SCHED_FUSED, rov.SCHED_OVERLAP):
+        print("block with other forms", causal, sched, flush=True)
+        y = torch.zeros_like(x)
+        mask = None if sched == rov.SCHED_FUSED else torch.zeros(rov.mask_shape(B, DIMS["H"], S), dtype=torch.int64, device="cuda")
+        torch.cuda.synchronize()
+        rov.block_forward(rov.make_block_weights(w), x, y, cfg, sched, seed, offset, mask, ws, main, side, opts=opts)
+        torch.cuda.synchronize()
+        ys.append(y)
+    assert torch.equal(ys[0], ys[1]) and torch.equal(ys[0], ys[2])
+    keep = OP.unpack_keep(OP.dropout_mask(seed, offset, B, DIMS["H"], S, p), S)
+    ref = _reference(_f64(x), {k: _f64(v) for k, v in w.items()}, {k: _f64(v) for k, v in around.items()}, pos.cpu().numpy(), keep, p, causal, 0.9, 0.5)
+    err = np.max(np.abs(_f64(ys[0]) - ref)) / np.max(np.abs(ref))
+    assert err <= 2e-2, err
+    plain = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    rov.block_forward(rov.make_block_weights(w), x, plain, cfg, rov.SCHED_FUSED, seed, offset, None, ws, main, side)
+    torch.cuda.synchronize()
+    assert np.max(np.abs(_f64(plain) - ref)) / np.max(np.abs(ref)) > 0.1     # the options are visible at this tolerance
+
+
+def test_block_options_at_their_defaults_are_the_plain_block():
+    B, S = 1, 200
+    x, w, _, _ = _setup(B, S, 72)
+    cfg = rov.make_block_cfg(*(DIMS[k] for k in ("H", "Hkv", "d", "hidden", "ffn")), 0.1)
+    ws = torch.empty(rov.block_workspace_bytes(cfg, B, S, 0), dtype=torch.uint8, device="cuda")
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for opts in (None, rov.make_block_opts(), rov.make_block_opts(rope=rov.make_rope_cfg(128, 500000.0))):
+        y = torch.zeros_like(x)
+        torch.cuda.synchronize()
+        rov.block_forward(rov.make_block_weights(w), x, y, cfg, rov.SCHED_FUSED, wl.SEED, 0, None, ws, main, side, opts=opts)
+        torch.cuda.synchronize()
+        outs.append(y)
+    assert torch.equal(outs[0], outs[1])
+    # the same rotation by another kernel: a sine's last bit may move a bf16 rounding of q or k
+    assert float((outs[0].double() - outs[2].double()).abs().max() / outs[0].double().abs().max()) <= 1e-2
+
+
+def test_fp8_block_with_post_norms():
+    # fp8 products: against the bf16 block of the same (dequantised) weights and options.  A quantiser moves a value by up to half a step,
+    # 2^-4 of it, 2^-4 / sqrt(3) = 3.6 % rms: the branches pass two (attention's) and two more (the feed-forward's, whose product of two
+    # factors counts one of them twice), sqrt(2) * 3.6 = 5.1 and sqrt(4) * 3.6 = 7.2 %, of a post-normed branch that is 0.7 * 0.58 (gate's rms) = 0.41 of a
+    # stream of rms 0.9: at most 0.41 * 8.8 % / 0.9 = 4 % rms, and as much of the largest value among 10^5 of the same distribution.
+    B, S = 1, 256
+    x, w, around, pos = _setup(B, S, 73)
+    names = ("wqkv", "wo", "wg", "wu", "wd")
+    dims = tuple({**DIMS, "ffn": 1024}[k] for k in ("H", "Hkv", "d", "hidden", "ffn"))
+    w = {k: (v[:1024].contiguous() if k in ("wg", "wu") else v[:, :1024].contiguous() if k == "wd" else v) for k, v in w.items()}
+    scale = {n: float(w[n].abs().max()) / 448.0 for n in names}
+    w8 = {n: ((w[n].float() / scale[n]).to(torch.float8_e4m3fn).view(torch.uint8) if n in names else w[n]) for n in w}
+    wb = {n: ((w8[n].view(torch.float8_e4m3fn).float() * scale[n]).to(torch.bfloat16) if n in names else w[n]) for n in w}
+    opts = rov.make_block_opts(positions=None, x_scale=0.9, h_scale=0.7, rows_per_gate=S, **around)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    ys = []
+    for dtype, weights in ((rov.BF16, rov.make_block_weights(wb)), (rov.FP8_E4M3, rov.make_block_weights(w8, scale))):
+        cfg = rov.make_block_cfg(*dims, 0.1, dtype=dtype, act_scale=[5.0 / 448, 4.0 / 448, 5.0 / 448, 2.0 / 448])
+        ws = torch.empty(rov.block_workspace_bytes(cfg, B, S, 0), dtype=torch.uint8, device="cuda")
+        y = torch.zeros_like(x)
+        torch.cuda.synchronize()
+        rov.block_forward(weights, x, y, cfg, rov.SCHED_FUSED, wl.SEED, 0, None, ws, main, side, opts=opts)
+        torch.cuda.synchronize()
+        ys.append(y.double())
+    d = (ys[0] - ys[1]).abs()
+    assert float(d.max() / ys[0].abs().max()) <= 8e-2 and float(d.square().mean().sqrt() / ys[0].square().mean().sqrt()) <= 6e-2
+
+
+def test_block_option_errors():
+    B, S = 1, 64
+    x, w, around, pos = _setup(B, S, 74)
+    cfg = rov.make_block_cfg(*(DIMS[k] for k in ("H", "Hkv", "d", "hidden", "ffn")), 0.0)
+    ws = torch.empty(rov.block_workspace_bytes(cfg, B, S, 0), dtype=torch.uint8, device="cuda")
+    y = torch.full_like(x, 3.0)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for bad in (rov.make_block_opts(rope=rov.make_rope_cfg(130, 1e4)), rov.make_block_opts(post1=around["post1"], rows_per_gate=48),
+                rov.make_block_opts(x_scale=float("nan")), rov.make_block_opts(gate2=around["gate2"], rows_per_gate=-1)):
+        with pytest.raises(rov.RovError) as e:
+            rov.block_forward(rov.make_block_weights(w), x, y, cfg, rov.SCHED_FUSED, 1, 0, None, ws, main, side, opts=bad)
+        assert e.value.code == rov.ERR_INVALID
+    torch.cuda.synchronize()
+    assert bool((y == 3.0).all())
+
+
+def test_training_tail_forward_and_back():
+    # hidden states -> norm around the branch -> loss over the vocabulary, and back; beside it queries turned by their positions and their
+    # gradient turned back.  Against automatic differentiation in 64 bits; every tensor between two operators is rounded to bf16 (half a
+    # step, 2^-8), the gradients pass three of them: relative errors of the whole tensors stay within 3 * 2^-8.
+    T, n, V = 300, 256, 2000
+    g = torch.Generator().manual_seed(75)
+    r = lambda *s: torch.randn(*s, generator=g).to(torch.bfloat16).cuda()
+    x, h, W = r(T, n), r(T, n), (r(V, n).float() * 0.1).to(torch.bfloat16)
+    w_pre, w_post, gate = 1 + 0.1 * r(n), 1 + 0.1 * r(n), r(3, n)
+    t = torch.randint(0, V, (T,), generator=g).cuda()
+    t[::7] = -100
+    dloss = torch.full((T,), 1.0 / T, device="cuda")
+    y, yn = rov.norm_residual(x, h, w_pre, w_post, gate, h_scale=0.5)
+    loss, lse = rov.linear_xent(yn, W, t)
+    dyn, dW = rov.linear_xent_bwd(yn, W, t, lse, dloss)
+    dy = torch.zeros_like(y)
+    dx, dh, dw_pre, dw_post, dgate = rov.norm_residual_bwd(y, h, dy, dyn, w_pre, w_post, gate, h_scale=0.5)
+
+    leaves = [v.double().requires_grad_() for v in (x, h, W, w_pre, w_post, gate)]
+    X, Hh, Wd, P, Q, G = leaves
+    rms = lambda v: v / torch.sqrt((v * v).mean(-1, keepdim=True) + 1e-5)
+    z = rms(X + 0.5 * G.repeat_interleave(T // 3, 0) * rms(Hh) * Q) * P
+    logits = z @ Wd.t()
+    keep = t != -100
+    want = (torch.logsumexp(logits, 1) - logits.gather(1, t.clamp(min=0)[:, None])[:, 0]) * keep
+    want.sum().div(T).backward()
+    assert float((loss.double() - want.detach()).abs().max()) <= 2.0 ** -8 * float(logits.detach().abs().max())
+    for name, got, leaf in zip(("x", "h", "W", "w_pre", "w_post", "gate"), (dx, dh, dW, dw_pre, dw_post, dgate), leaves):
+        err = float((got.double() - leaf.grad).norm() / leaf.grad.norm())
+        assert err <= 3 * 2.0 ** -8, (name, err)
+
+    cfg = rov.make_rope_cfg(64, 10000.0, layout=rov.ROPE_HALVES)
+    q = r(1, T, 4, 64)
+    back = rov.rope(cfg, rov.rope(cfg, q), backward=True)       # two roundings, |a| + |b| <= sqrt(2) of the pair's length
+    assert float((back.double() - q.double()).norm() / q.double().norm()) <= 2 * 2.0 ** -8
