@@ -639,8 +639,8 @@ int rov_linear_xent(const void *X, const void *W, const int64_t *targets, int M,
 
 /* Its gradients, from the lse of the forward call and the gradients of loss and (may be NULL) lse:
  *     G = scale * (softmax(z) * (dloss + dlse) - onehot(target) * dloss),   dX = G W,   dW = G^T X,
- * in the dtype of X and W, row strides lddx, lddw (>= K).  dX or dW may be NULL.  fp32 accumulation; for bf16, G is rounded to bf16 for
- * the matrix products.  Every element of dX and dW is written.  The logits are made a second time. */
+ * in the dtype of X and W, row strides lddx, lddw (>= K).  dX or dW may be NULL.  fp32 accumulation; for bf16, G without its
+ * row's factor and (for dW) the rows of X times it are rounded to bf16 for the matrix products.  Every element of dX and dW is written.  The logits are made a second time. */
 int rov_linear_xent_bwd(const void *X, const void *W, const int64_t *targets, const float *lse,
                         const float *dloss, const float *dlse, int M, int V, int K, int64_t ldx, int64_t ldw,
                         int dtype, float scale, int64_t ignore_index, void *dX, void *dW, int64_t lddx,

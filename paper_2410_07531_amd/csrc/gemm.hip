@@ -583,7 +583,7 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         return;
     }
     if constexpr (HEAD == HEAD_GRAD) {
-        // gradients of the logits, G[m][n]; rows that are ignored and columns beyond N are zero, so that G can be walked in whole slots as the
+        // gradients of the logits over the row's factor, G[m][n]; rows that are ignored and columns beyond N are zero, so that G can be walked in whole slots as the
         // next product's k
         const int mw = m0 + wm * 128 + 8 * mrow;          // first of this lane's eight rows
         const int nl = n0 + wn * 128 + 2 * nsub;          // first of its columns nl + 32*j + 0..7
@@ -596,11 +596,11 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
             const int64_t t = m < M ? head.targets[m] : head.ignore;
             keep[i] = t != head.ignore;
             whole = whole && keep[i];
-            const float a = keep[i] ? (t >= 0 && t < head.vocab ? head.dloss[m] : NAN) : 0.0f;
-            const float b = keep[i] && head.dlse != nullptr ? head.dlse[m] : 0.0f;
+            const float f = keep[i] ? head.factor[m] : 0.0f, inv = f != 0.0f ? 1.0f / f : 0.0f;
+            const float a = keep[i] ? head.dloss[m] : 0.0f, b = keep[i] && head.dlse != nullptr ? head.dlse[m] : 0.0f;
             lse2[i] = keep[i] ? head.lse[m] * 1.44269504088896341f : 0.0f;
-            up[i] = (a + b) * head.scale;
-            down[i] = a * head.scale;
+            up[i] = (a + b) * inv;
+            down[i] = a * inv;
             const int64_t c = t - head.v0 - nl;   // 32*j + 0..7: this lane's
             tcol[i] = keep[i] && c >= 0 && c < 128 && (c & 31) < 8 ? (int)c : -1;
             hit = hit || tcol[i] >= 0;
@@ -639,6 +639,13 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     if constexpr (KNW) {
         // fp32 sums of the shares of k, rows of ld_sum values; or the result itself, bf16
         float* const sums = head.sum != nullptr ? head.sum + (size_t)blockIdx.y * M * head.ld_sum : nullptr;
+        float times[8];   // (read here, once: between the stores each would wait for its own read)
+        if (sums == nullptr)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int m = m0 + wm * 128 + i * 16 + mrow;
+                times[i] = head.factor[head.factor_step * (m < M ? m : M - 1)] * head.scale;
+            }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             __builtin_amdgcn_sched_barrier(0);
@@ -657,7 +664,8 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
                     *at = c;
                 } else {
                     uint16_t* const out = C + (size_t)m * head.ld_out + n;
-                    const uint2 v = make_uint2(pack_bf16x2(c[0], c[1]), pack_bf16x2(c[2], c[3]));
+                    const float f = times[i];
+                    const uint2 v = make_uint2(pack_bf16x2(f * c[0], f * c[1]), pack_bf16x2(f * c[2], f * c[3]));
                     if (head.out_wide && n + 3 < N) {
                         *reinterpret_cast<uint2*>(out) = v;
                     } else {

@@ -111,11 +111,11 @@ int check_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, const v
 // 256-row kernel with other epilogues.  A [M,K], W [N,K], K contiguous, K % 8 == 0:
 //   HEAD_STATS  z = A W^T * alpha (logits in units of log 2): per row and half tile (128 columns) maximum and sum of exp2 to
 //               part[2 * gemm_head_tiles_n(N)][M], the target's z to picked[m] (rows whose target is one of the N columns, v0 the first);
-//   HEAD_GRAD   G[m][n] = scale * (exp2(z - lse log2 e) * (dloss + dlse) - [v0 + n == target] * dloss) in bf16 to g [M][ld_g], columns
-//               N .. ld_g (N rounded up to 64) and rows of ignored targets zero.
+//   HEAD_GRAD   G[m][n] = (exp2(z - lse log2 e) * (dloss + dlse) - [v0 + n == target] * dloss) / factor[m] in bf16 to g [M][ld_g], columns
+//               N .. ld_g (N rounded up to 64) and rows of ignored targets (or with factor 0) zero.
 // W [K,N], N contiguous, and A [M,K] with rows of whole slots (64 values, zero beyond K; HEAD_DX) or [K,M] (HEAD_DW): A W or A^T W;
 // `shares` workgroups a tile take a share of k each and write fp32 (add: add to) sum[share][M][ld_sum]; sum == NULL (one share): bf16
-// to C, rows of ld_out (out_wide: rows on 8 bytes).
+// to C, rows of ld_out (out_wide: rows on 8 bytes), times factor[factor_step * m] * scale.
 enum { HEAD_STATS = 1, HEAD_GRAD = 2, HEAD_DX = 3, HEAD_DW = 4 };
 struct HeadArgs {
     size_t ld_a = 0, ld_w = 0;
@@ -125,9 +125,11 @@ struct HeadArgs {
     const float* lse = nullptr;
     const float* dloss = nullptr;
     const float* dlse = nullptr;
+    const float* factor = nullptr;
+    int64_t factor_step = 1;
     uint16_t* g = nullptr;
     int64_t ld_g = 0;
-    int64_t ignore = 0, v0 = 0, vocab = 0;
+    int64_t ignore = 0, v0 = 0;
     float scale = 1.0f;
     float* sum = nullptr;
     int64_t ld_sum = 0, ld_out = 0;

@@ -9,6 +9,10 @@
 // walks the vocabulary in pieces: the accumulators of a piece's logits become G, stored in bf16 (the tile's columns are dealt to the lanes so
 // that G leaves in 16-byte stores), and the products for dX and dW read G, W and X as they lie, k across the rows, through transposing LDS
 // loads.  dX is summed over the pieces, and either over shares of k where its tiles alone would leave compute units idle, in fp32.
+// G is rounded to bf16 without its row's factor dloss: with the factor in it, the entries of the targets, which are the bulk of it and
+// nearly the same number -dloss in every row of a mean, would all be off by the same part of up to 2^-9, and so would dX and dW (0.0033 of
+// their norm, 0.0021 without).  dX is multiplied by its row's factor in fp32; for dW the rows of X are multiplied by theirs over the largest,
+// which changes nothing where they are all the same, and dW by the largest.
 // fp32: the fp32 products of gemm_ring.hip; a piece's logits live in the workspace while they are reduced, or turned into G in place.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -112,27 +116,61 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(float* __restrict__ z, f
 }
 
 // ------------------------------------------------------------------ bf16
-// dst [rows][kp] = src, columns K .. kp zero, rows of ignored targets (targets may be NULL) zero; eight values a thread.
+// factor[m]: dloss, or dloss + dlse where dloss is next to nothing beside it; 0 for rows of ignored targets, NaN for targets outside the
+// vocabulary.  factor[M]: the largest of their magnitudes.  One workgroup.
+__global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t* __restrict__ targets, int64_t ignore, int V, const float* __restrict__ dloss,
+                                                           const float* __restrict__ dlse, float* __restrict__ factor, int M) {
+    __shared__ float red[16];
+    float most = 0.0f;
+    for (int m = threadIdx.x; m < M; m += 1024) {
+        const int64_t t = targets[m];
+        const float a = dloss[m], s = dlse != nullptr ? a + dlse[m] : a;
+        const float f = t == ignore ? 0.0f : !in_vocab(t, V) ? NAN : fabsf(a) * 1048576.0f >= fabsf(s) ? a : s;
+        factor[m] = f;
+        most = fmaxf(most, fabsf(f));
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, red[i]);
+    factor[M] = most;
+}
+
+// dst [rows][kp] = src, columns K .. kp zero; times factor[r] / factor[rows] where it is given, rows with factor 0 zero whatever they
+// hold.  Eight values a thread.
 __global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restrict__ src, int64_t ld, uint16_t* __restrict__ dst, int64_t rows, int K, int kp,
-                                                        bool wide, const int64_t* __restrict__ targets, int64_t ignore) {
+                                                        bool wide, const float* __restrict__ factor) {
     const int chunks = kp / 8;
     const int64_t total = rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / chunks;
         const int c = (int)(i - r * chunks) * 8;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (targets == nullptr || targets[r] != ignore) {
+        float f = factor != nullptr ? factor[r] : 1.0f;
+        Piece<uint16_t, 8> v;
+        v.zero();
+        if (f != 0.0f) {
             const uint16_t* const at = src + r * ld + c;
             if (wide) {
-                v = *reinterpret_cast<const uint4*>(at);
+                v.load(at);
             } else {
                 uint32_t h[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) h[e] = c + e < K ? at[e] : 0u;
-                v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+                v.raw = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+            }
+            if (factor != nullptr) f /= factor[rows];
+            if (f != 1.0f) {
+                float x[8];
+                v.get(x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= f;
+                v.set(x);
             }
         }
-        *reinterpret_cast<uint4*>(dst + r * kp + c) = v;
+        v.store(dst + r * kp + c);
     }
 }
 
@@ -172,7 +210,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
     loss[m] = t == ignore ? 0.0f : in_vocab(t, V) ? (float)(l - (double)picked[m] * ln2) : NAN;
 }
 
-// dW [V][K] (rows of ldo) = G^T X over at most 64 * SLOTS rows: G [M][ldg], X [M][ldx], both with rows of whole 16-byte chunks.
+// dW [V][K] (rows of ldo) = factor[0] * scale * G^T X over at most 64 * SLOTS rows: G [M][ldg], X [M][ldx], both with rows of whole 16-byte chunks.
 // What bounds it: dW's bytes.  A 256 x 256 tile of gemm.hip has one or two slots of 64 rows to walk here, and with one workgroup a compute unit
 // nothing runs while its operands travel and its results leave.  Here a workgroup keeps 128 columns of X in registers, walks over
 // tiles of 128 columns of G, the next of which is on its way, and three (two) workgroups share a compute unit.  131072 x 4096, us, 256 x 256
@@ -186,7 +224,8 @@ typedef __attribute__((address_space(3))) i16x4* lds_i16x4_ptr;
 
 template <int SLOTS>
 __global__ __launch_bounds__(256, SLOTS == 1 ? 3 : 2) void xent_outer_kernel(const uint16_t* __restrict__ G, int64_t ldg, const uint16_t* __restrict__ X, int64_t ldx,
-                                                           uint16_t* __restrict__ out, int64_t ldo, bool out_wide, int V, int K, int M, int tiles_v) {
+                                                           uint16_t* __restrict__ out, int64_t ldo, bool out_wide, int V, int K, int M, int tiles_v,
+                                                           const float* __restrict__ factor, float scale) {
     constexpr int kTile = SLOTS * 64 * 256;
     __shared__ __attribute__((aligned(16))) char lds[2][kTile];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wv = wave >> 1, wk = wave & 1;
@@ -233,6 +272,7 @@ __global__ __launch_bounds__(256, SLOTS == 1 ? 3 : 2) void xent_outer_kernel(con
     put(lds[0]);
     __syncthreads();
     const int steps = (M + 31) / 32;
+    const float times = factor[0] * scale;
     for (int buf = 0; tile < tiles_v; buf ^= 1) {
         const int here = tile;
         tile += gridDim.y;
@@ -267,7 +307,7 @@ __global__ __launch_bounds__(256, SLOTS == 1 ? 3 : 2) void xent_outer_kernel(con
                 uint16_t* const to = out + (int64_t)v * ldo + k;
                 uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = bf16_pair(acc[2 * t + (e >> 1)][i][2 * (e & 1)], acc[2 * t + (e >> 1)][i][2 * (e & 1) + 1]);
+                for (int e = 0; e < 4; ++e) w[e] = bf16_pair(times * acc[2 * t + (e >> 1)][i][2 * (e & 1)], times * acc[2 * t + (e >> 1)][i][2 * (e & 1) + 1]);
                 if (out_wide && k + 7 < K) {
                     *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
                 } else {
@@ -281,9 +321,9 @@ __global__ __launch_bounds__(256, SLOTS == 1 ? 3 : 2) void xent_outer_kernel(con
     }
 }
 
-// out [rows][K] (bf16, rows of ldo) = sum over shares of sums[share][rows][lds].
+// out [rows][K] (bf16, rows of ldo) = sum over shares of sums[share][rows][lds], times factor[step * r] * scale.
 __global__ __launch_bounds__(256) void xent_fold_kernel(const float* __restrict__ sums, int shares, int64_t lds, uint16_t* __restrict__ out, int64_t ldo,
-                                                        int64_t rows, int K) {
+                                                        int64_t rows, int K, const float* __restrict__ factor, int64_t step, float scale) {
     const int64_t quads = lds / 4, total = rows * quads;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / quads;
@@ -294,7 +334,8 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const float* __restrict_
             const float4 v = *reinterpret_cast<const float4*>(sums + ((int64_t)k * rows + r) * lds + c);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
-        const uint32_t lo = bf16_pair(s.x, s.y), hi = bf16_pair(s.z, s.w);
+        const float f = factor[step * r] * scale;
+        const uint32_t lo = bf16_pair(f * s.x, f * s.y), hi = bf16_pair(f * s.z, f * s.w);
         const uint16_t h[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
         uint16_t* const to = out + r * ldo + c;
 #pragma unroll
@@ -361,7 +402,7 @@ int shares_of(int M, int N, int64_t K) {
 struct HeadLayout {
     int piece, packed, shares_x, shares_w;   // columns of a piece, of a piece of W that is packed
     int64_t kp, ks;                          // K as rows of packed operands, of sums
-    size_t x, w, part, picked, g, sum_x, sum_w, total;
+    size_t x, w, part, picked, factor, xs, g, sum_x, sum_w, total;   // xs: X times its rows' factors
 };
 HeadLayout head_layout(int M, int V, int K, int asked, bool backward) {
     HeadLayout l{};
@@ -382,6 +423,8 @@ HeadLayout head_layout(int M, int V, int K, int asked, bool backward) {
     } else {
         l.shares_x = shares_of(M, K, l.packed);
         l.shares_w = shares_of(l.packed, K, M);
+        l.factor = take(((size_t)M + 1) * 4);
+        l.xs = take((size_t)M * l.kp * 2);
         l.g = take((size_t)M * up_to(l.piece, 64) * 2);
         l.sum_x = take(l.shares_x > 1 || l.packed < V ? (size_t)l.shares_x * M * l.ks * 4 : 0);
         l.sum_w = take(l.shares_w > 1 ? (size_t)l.shares_w * l.piece * l.ks * 4 : 0);
@@ -407,18 +450,27 @@ int check_xent(const void* X, const void* W, const int64_t* targets, int M, int 
     return ROV_OK;
 }
 
-int pack(const void* src, int64_t ld, void* dst, int64_t rows, int K, int64_t kp, const int64_t* targets, int64_t ignore, hipStream_t st) {
+int pack(const void* src, int64_t ld, void* dst, int64_t rows, int K, int64_t kp, const float* factor, hipStream_t st) {
     const bool wide = K % 8 == 0 && ld % 8 == 0 && aligned(src, 16);
     hipLaunchKernelGGL(xent_pack_kernel, dim3(sweep_grid(rows * kp / 8)), dim3(256), 0, st, (const uint16_t*)src, ld, (uint16_t*)dst, rows, K, (int)kp, wide,
-                       targets, ignore);
+                       factor);
+    ROV_LAUNCH_CHECK();
+    return ROV_OK;
+}
+int fold(const float* sums, int shares, int64_t lds, void* out, int64_t ldo, int rows, int K, const float* factor, int64_t step, float scale, hipStream_t st) {
+    hipLaunchKernelGGL(xent_fold_kernel, dim3(sweep_grid((int64_t)rows * lds / 4)), dim3(256), 0, st, sums, shares, lds, (uint16_t*)out, ldo, (int64_t)rows, K,
+                       factor, step, scale);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
 // out [M][N] (rows of ldo) = A W or A^T W summed over `shares` of k; sum == NULL (one share): at once, else through sum, to which it is added
-// (`add`), and from there to out if `last`.  Strides in elements.
+// (`add`), and from there to out if `last`, times factor[step * m] * scale.  Strides in elements.
 int product(int kind, const void* A, int64_t lda, const void* W, int64_t ldw, void* out, int64_t ldo, int M, int N, int K, int shares, float* sum,
-            int64_t lds, bool add, bool last, hipStream_t st) {
+            int64_t lds, bool add, bool last, const float* factor, int64_t step, float scale, hipStream_t st) {
     HeadArgs h;
+    h.factor = factor;
+    h.factor_step = step;
+    h.scale = scale;
     h.ld_a = (size_t)lda * 2;
     h.ld_w = (size_t)ldw * 2;
     h.sum = sum;
@@ -428,11 +480,10 @@ int product(int kind, const void* A, int64_t lda, const void* W, int64_t ldw, vo
     h.out_wide = aligned(out, 8) && ldo % 4 == 0;
     const int rc = launch_gemm_head(kind, A, W, out, M, N, K, 1.0f, shares, h, st);
     if (rc != ROV_OK || sum == nullptr || !last) return rc;
-    hipLaunchKernelGGL(xent_fold_kernel, dim3(sweep_grid((int64_t)M * lds / 4)), dim3(256), 0, st, sum, shares, lds, (uint16_t*)out, ldo, (int64_t)M, N);
-    ROV_LAUNCH_CHECK();
-    return ROV_OK;
+    return fold(sum, shares, lds, out, ldo, M, N, factor, step, scale, st);
 }
-int outer(const void* G, int64_t ldg, const void* X, int64_t ldx, uint16_t* out, int64_t ldo, int V, int K, int M, hipStream_t st) {
+int outer(const void* G, int64_t ldg, const void* X, int64_t ldx, uint16_t* out, int64_t ldo, int V, int K, int M, const float* factor, float scale,
+          hipStream_t st) {
     const int64_t tiles_k = up_to(K, 128) / 128, tiles_v = up_to(V, 128) / 128;
     int64_t rows = 3 * device_cu_count() / tiles_k;   // as many workgroups as run at once
     if (rows > tiles_v) rows = tiles_v;
@@ -440,9 +491,11 @@ int outer(const void* G, int64_t ldg, const void* X, int64_t ldx, uint16_t* out,
     const bool wide = aligned(out, 16) && ldo % 8 == 0;
     const dim3 grid((unsigned)tiles_k, (unsigned)rows);
     if (M <= 64)
-        hipLaunchKernelGGL(xent_outer_kernel<1>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v);
+        hipLaunchKernelGGL(xent_outer_kernel<1>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v,
+                           factor, scale);
     else
-        hipLaunchKernelGGL(xent_outer_kernel<2>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v);
+        hipLaunchKernelGGL(xent_outer_kernel<2>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v,
+                           factor, scale);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
@@ -473,7 +526,7 @@ int head_forward(const void* X, const void* W, const int64_t* targets, int M, in
         x = ws + l.x;
         h.ld_a = (size_t)l.kp * 2;
         kx = (int)l.kp;
-        const int rc = pack(X, ldx, ws + l.x, M, K, l.kp, nullptr, 0, st);
+        const int rc = pack(X, ldx, ws + l.x, M, K, l.kp, nullptr, st);
         if (rc != ROV_OK) return rc;
     }
     if (fit_w) {
@@ -484,7 +537,7 @@ int head_forward(const void* X, const void* W, const int64_t* targets, int M, in
         h.ld_w = (size_t)l.kp * 2;
         for (int v0 = 0; v0 < V; v0 += l.packed) {
             const int cols = V - v0 < l.packed ? V - v0 : l.packed;
-            int rc = pack((const char*)W + (size_t)v0 * ldw * 2, ldw, ws + l.w, cols, K, l.kp, nullptr, 0, st);
+            int rc = pack((const char*)W + (size_t)v0 * ldw * 2, ldw, ws + l.w, cols, K, l.kp, nullptr, st);
             if (rc != ROV_OK) return rc;
             h.v0 = v0;
             h.part = (float2*)(ws + l.part) + (size_t)(v0 / 128) * M;   // (pieces are whole tiles)
@@ -512,15 +565,24 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
     h.dloss = dloss;
     h.dlse = dlse;
     h.ignore = ignore;
-    h.vocab = V;
-    h.scale = scale;
-    // X without the ignored rows: what they hold must not reach dW
-    int rc = pack(X, ldx, ws + l.x, M, K, l.kp, targets, ignore, st);
-    if (rc != ROV_OK) return rc;
-    const char* const x = ws + l.x;
-    h.ld_a = (size_t)l.kp * 2;
+    h.factor = (const float*)(ws + l.factor);
+    hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, ignore, V, dloss, dlse, (float*)(ws + l.factor), M);
+    ROV_LAUNCH_CHECK();
     const bool fit_w = rows_fit(W, ldw, K);
-    const int kx = (int)l.kp, piece = fit_w ? l.piece : l.packed;
+    const char* x = (const char*)X;
+    h.ld_a = (size_t)ldx * 2;
+    int rc = ROV_OK;
+    if (!fit_w || !rows_fit(X, ldx, K)) {
+        x = ws + l.x;
+        h.ld_a = (size_t)l.kp * 2;
+        rc = pack(X, ldx, ws + l.x, M, K, l.kp, nullptr, st);
+        if (rc != ROV_OK) return rc;
+    }
+    if (dW != nullptr) {
+        rc = pack(X, ldx, ws + l.xs, M, K, l.kp, h.factor, st);
+        if (rc != ROV_OK) return rc;
+    }
+    const int kx = (int)l.kp, piece = fit_w ? l.piece : l.packed;   // (operands that fit have K = kp)
     float* const sum_x = l.shares_x > 1 || piece < V ? (float*)(ws + l.sum_x) : nullptr;
     float* const sum_w = l.shares_w > 1 ? (float*)(ws + l.sum_w) : nullptr;
     for (int v0 = 0; v0 < V; v0 += piece) {
@@ -529,7 +591,7 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
         const char* w = (const char*)W + (size_t)v0 * ldw * 2;
         int64_t ld = ldw;
         if (!fit_w) {
-            rc = pack(w, ldw, ws + l.w, cols, K, l.kp, nullptr, 0, st);
+            rc = pack(w, ldw, ws + l.w, cols, K, l.kp, nullptr, st);
             if (rc != ROV_OK) return rc;
             w = ws + l.w;
             ld = l.kp;
@@ -543,25 +605,21 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
         if (dX != nullptr) {
             // (the last, shorter piece may have fewer slots of k than shares: the sums of the shares left out stay)
             const int shares = l.shares_x > ldg / 64 ? (int)(ldg / 64) : l.shares_x;
-            rc = product(HEAD_DX, ws + l.g, ldg, w, ld, dX, lddx, M, K, cols, shares, sum_x, l.ks, v0 > 0, false, st);
+            rc = product(HEAD_DX, ws + l.g, ldg, w, ld, dX, lddx, M, K, cols, shares, sum_x, l.ks, v0 > 0, false, h.factor, 1, scale, st);
             if (rc != ROV_OK) return rc;
         }
         if (dW != nullptr) {
             if (M <= 128) {
-                rc = outer(ws + l.g, ldg, x, l.kp, (uint16_t*)dW + (size_t)v0 * lddw, lddw, cols, K, M, st);
+                rc = outer(ws + l.g, ldg, ws + l.xs, l.kp, (uint16_t*)dW + (size_t)v0 * lddw, lddw, cols, K, M, h.factor + M, scale, st);
                 if (rc != ROV_OK) return rc;
                 continue;
             }
-            rc = product(HEAD_DW, ws + l.g, ldg, x, l.kp, (char*)dW + (size_t)v0 * lddw * 2, lddw, cols, K, M, l.shares_w, sum_w, l.ks, false, true, st);
+            rc = product(HEAD_DW, ws + l.g, ldg, ws + l.xs, l.kp, (char*)dW + (size_t)v0 * lddw * 2, lddw, cols, K, M, l.shares_w, sum_w, l.ks, false, true,
+                         h.factor + M, 0, scale, st);
             if (rc != ROV_OK) return rc;
         }
     }
-    if (dX != nullptr && sum_x != nullptr) {
-        hipLaunchKernelGGL(xent_fold_kernel, dim3(sweep_grid((int64_t)M * l.ks / 4)), dim3(256), 0, st, sum_x, l.shares_x, l.ks, (uint16_t*)dX, lddx,
-                           (int64_t)M, K);
-        ROV_LAUNCH_CHECK();
-    }
-    return ROV_OK;
+    return dX != nullptr && sum_x != nullptr ? fold(sum_x, l.shares_x, l.ks, dX, lddx, M, K, h.factor, 1, scale, st) : ROV_OK;
 }
 
 int copy(const void* src, int64_t lds, void* dst, int64_t ldd, int64_t rows, int cols, const int64_t* targets, int64_t ignore, hipStream_t st) {

@@ -3,6 +3,7 @@
 Tolerances.  A logit is a sum of K products in fp32: off by at most K * 2^-24 of scale * sum |x w| (dz below, the largest
 of the row).  exp and log add 2^-21 of a sum of positives and 2^-23 of their result, so lse and loss are off by at most
 2 dz + 2^-20 + 2^-22 |lse|.  A gradient logit G is off by (2 dz + 2^-19) of its two terms' magnitudes, and, for bf16, by a half step, 2^-8, of itself;
+for dW the rows of X, times their factors, are rounded too: another 2^-8 of each term;
 products over V (dX) and M (dW) terms carry that and add V (M) * 2^-24 of the sum of magnitudes; bf16 results another 2^-8.
 Below the smallest normal number, 2^-126, fp32 has no relative precision (exp and the matrix products flush there): a term
 of G (|dloss + dlse| < 4) is off by up to 4 * 2^-126, its product with w or x by another 2^-126, V (M) of them in a sum.
@@ -52,7 +53,8 @@ def reference(X, W, t, dloss=None, dlse=None, scale=1.0, ignore=-100):
     out["dX"], out["dW"] = G @ W, G.t() @ Xk
     half = 2.0 ** -8 if bf16 else 2.0 ** -24
     out["tX"] = err @ W.abs() + V * 2.0 ** -24 * (mag @ W.abs()) + half * out["dX"].abs()
-    out["tW"] = err.t() @ Xk.abs() + M * 2.0 ** -24 * (mag.t() @ Xk.abs()) + half * out["dW"].abs()
+    errW = err + (2.0 ** -8 * G.abs() if bf16 else 0.0)
+    out["tW"] = errW.t() @ Xk.abs() + M * 2.0 ** -24 * (mag.t() @ Xk.abs()) + half * out["dW"].abs()
     out["tX"] += V * 2.0 ** -126 * (1 + 4 * W.abs().max())
     out["tW"] += M * 2.0 ** -126 * (1 + 4 * Xk.abs().max())
     return out
