@@ -39,6 +39,7 @@
 // fp8 rows off 16 bytes, fp8 [K,N] weights, operands beyond 32-bit offsets) takes a small
 // LDS-tiled VALU kernel that is correct for any shape.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include "fp8_device.h"
@@ -176,6 +177,20 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return *reinterpret_cast<uint32_t*>(&h);
 }
 
+// A lane's value and that of the lane 16 (32) away, in an order that both lanes share: two vector moves, where a shuffle would go
+// through the LDS unit and be waited for.
+template <int D>
+__device__ __forceinline__ f32x2 exchanged(float v) {
+    const uint32_t u = __float_as_uint(v);
+    if constexpr (D == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+    }
+}
+
 // What the epilogue does with the bf16 side input R[m][n] (four consecutive n per lane):
 // EPI_ADD: C = acc + R (residual connection); EPI_SILU_MUL: C = silu(R) * acc (SwiGLU: R is the
 // gate projection, acc the up projection, so the activation costs no kernel and no extra pass).
@@ -216,7 +231,7 @@ __device__ __forceinline__ void epilogue_combine(int epi, uint2 r, float& c0, fl
 // one select a load, and read zeros) and any number of output columns.
 // HEAD: the products of the loss over the vocabulary (HeadArgs; bf16, rows of any stride): the epilogue keeps the row statistics of
 // the tile's logits (HEAD_STATS), or the gradients of its logits (HEAD_GRAD), or stores or adds up fp32 sums (HEAD_DX, HEAD_DW).
-// HEAD_DX: the second operand lies as [K, N] (rows of k), HEAD_DW: both do.  Such an operand's part of a slot is 64 rows of k by 256
+// HEAD_DX: the second operand lies as [K, N] (rows of k), HEAD_DW: both do.  Such an operand's part of a slot is 64 rows of k by the tile's
 // columns; fragments come by the transposing LDS load, two a fragment, with the k order of the other operand's.
 template <int NJ, bool FP8, bool DUAL = false, bool OUT8 = false, bool RAGGED = false, int HEAD = 0>
 __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char* __restrict__ Wt,
@@ -226,7 +241,7 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
                                           const int wave, float alpha2 = 1.0f, float out_inv = 1.0f,
                                           const HeadArgs& head = HeadArgs{}) {
     static_assert(!OUT8 || DUAL, "e4m3 output exists in the dual form only");
-    static_assert(HEAD == 0 || (!FP8 && !DUAL && (HEAD <= HEAD_STATS || NJ == 8)), "the loss's products: plain bf16, 256 columns");
+    static_assert(HEAD == 0 || (!FP8 && !DUAL && NJ % 4 == 0), "the loss's products: plain bf16, 256 or 128 columns");
     static_assert(!RAGGED || (!FP8 && !DUAL), "rows off 128 bytes: the plain bf16 product only");
     constexpr bool MIXED = DUAL && NJ % 4 != 0;   // gate and up rows in every weight block
     const int wm = wave >> 1, wn = wave & 1;
@@ -299,7 +314,7 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     }
     // bytes of k that a row holds from the base on (the last row's end bounds the operand)
     const size_t k_bytes = KNW ? (size_t)ns * kRow : ld_bytes;
-    // 16-byte chunk swizzle of an LDS row of 256 columns: lanes that the transposing load serves together read rows {0-3, 8-11} (+4, +16) x 32
+    // 16-byte chunk swizzle of an LDS row of columns: lanes that the transposing load serves together read rows {0-3, 8-11} (+4, +16) x 32
     // bytes, so the 32-byte groups of those rows have to differ
     auto swz_kn = [](int row) { return ((row & 3) | (((row >> 3) & 1) << 2)) << 1; };
     const int rows_a = M - m0 < BM ? M - m0 : BM;
@@ -309,8 +324,8 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     for (int j = 0; j < 8; ++j) {
         const int row = (wave + 4 * j) * 8 + (lane >> 3);
         const int chunk = (lane & 7) ^ swz(row);
-        // HEAD_GRAD: LDS row 128*h + 16*i + r holds activation row 128*h + 8*r + i, and weight row 128*h + 32*j + 16*k + 4*g + e (k = 0, 1) weight
-        // row 128*h + 32*j + 8*g + 4*k + e, so that a lane ends up with eight consecutive rows and four times eight consecutive columns of the
+        // HEAD_GRAD: LDS row 128*h + 16*i + r holds activation row 128*h + 8*r + i, and weight row 32*j + 16*k + 4*g + e (k = 0, 1) weight
+        // row 32*j + 8*g + 4*k + e, so that a lane ends up with eight consecutive rows and groups of eight consecutive columns of the
         // tile, and the four lanes of a row with 32
         const int arow = HEAD == HEAD_GRAD ? (row & 128) | ((row & 15) << 3) | ((row >> 4) & 7) : row;
         const int ra = arow < rows_a ? arow : rows_a - 1;   // rows past the edge are never stored
@@ -318,15 +333,16 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         // mixed: LDS rows [16*b, +8) are gate rows of output columns 8*b .., the next 8 the up rows
         const int wcol = MIXED ? (row >> 4) * 8 + (row & 7)
                                : DUAL ? (row / (16 * NJ)) * (8 * NJ) + row % (8 * NJ) : row;
-        const int wrow = HEAD == HEAD_GRAD ? (row & (128 + 64 + 32)) | (((row >> 2) & 3) << 3) | (((row >> 4) & 1) << 2) | (row & 3) : wcol;
+        const int wrow = HEAD == HEAD_GRAD ? (row & ~31) | (((row >> 2) & 3) << 3) | (((row >> 4) & 1) << 2) | (row & 3) : wcol;
         const int rw = wrow < rows_w ? wrow : rows_w - 1;
         voff_a[j] = (uint32_t)((size_t)ra * ld_a) + (uint32_t)(chunk * 16);
         if (j < NJ) voff_w[j] = (uint32_t)((size_t)rw * ld_w) + (uint32_t)(chunk * 16);
-        if constexpr (KNW) {   // a load is two rows of k
-            const int krow = (wave + 4 * j) * 2 + (lane >> 5);
-            const uint32_t at = (uint32_t)(((lane & 31) ^ swz_kn(krow)) * 16);
-            if (KNA) voff_a[j] = (uint32_t)krow * (uint32_t)ld_a + at;
-            voff_w[j] = (uint32_t)krow * (uint32_t)ld_w + at;
+        if constexpr (KNW) {   // a load is two rows of k of 256 columns, or four of 128
+            const int arow_k = (wave + 4 * j) * 2 + (lane >> 5);
+            if (KNA) voff_a[j] = (uint32_t)arow_k * (uint32_t)ld_a + (uint32_t)(((lane & 31) ^ swz_kn(arow_k)) * 16);
+            constexpr int C = 4 * NJ;   // chunks of a row
+            const int wrow_k = (wave + 4 * j) * (64 / C) + lane / C;
+            if (j < NJ) voff_w[j] = (uint32_t)wrow_k * (uint32_t)ld_w + (uint32_t)(((lane % C) ^ swz_kn(wrow_k)) * 16);
         }
     }
     const char* a_panel = A + (KNA ? (size_t)m0 * ESZ : (size_t)m0 * ld_a);
@@ -450,19 +466,18 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
     } else {
         i32x4 af[2][8], wf[2][NJ];   // fragments of the two k-steps of a slot
         // [K, N] operands: lane 16g + 4r + s supplies rows 32h + 8g (+4) + r, columns 4s of the block, and receives its own column's values
-        const int kn_r = (lane >> 2) & 3, kn_g = lane >> 4;
-        const int kn_lane = (8 * kn_g + kn_r) * 512 + (lane & 3) * 8, kn_f = kn_r | ((kn_g & 1) << 2);
-        auto read_kn = [&](const char* base, int h, int b) {
-            const char* const at = base + kn_lane + ((b ^ kn_f) << 5) + h * 32 * 512;
+        const int kn_r = (lane >> 2) & 3, kn_g = lane >> 4, kn_f = kn_r | ((kn_g & 1) << 2);
+        auto read_kn = [&](const char* base, int pitch, int h, int b) {
+            const char* const at = base + (32 * h + 8 * kn_g + kn_r) * pitch + ((b ^ kn_f) << 5) + (lane & 3) * 8;
             const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)at);
-            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + 4 * 512));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + 4 * pitch));
             return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         };
         auto read_frag = [&](int h, const char* slot, int f /*0..7 = A block, 8..7+NJ = W block*/) {
             if (KNA && f < 8)
-                af[h][f] = read_kn(slot + wm * 256, h, f);
+                af[h][f] = read_kn(slot + wm * 256, 512, h, f);
             else if (KNW && f >= 8)
-                wf[h][f - 8] = read_kn(slot + BM * kRow + wn * 256, h, f - 8);
+                wf[h][f - 8] = NJ == 8 ? read_kn(slot + BM * kRow + wn * 256, 512, h, f - 8) : read_kn(slot + BM * kRow, 256, h, 4 * wn + f - 8);
             else if (f < 8)
                 af[h][f] = *reinterpret_cast<const i32x4*>(slot + a_base + f * 16 * kRow + foff[h]);
             else
@@ -544,6 +559,13 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         // target's logit where it is one of them
         const int nw = n0 + wn * 16 * NJ;
         const bool edge = nw + 16 * NJ > N;
+        int tcol[8];   // the targets' columns within this wave (read here, all at once: between the rows each would wait for its own read)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int m = m0 + wm * 128 + i * 16 + mrow;
+            const int64_t t = m < M ? head.targets[m] - head.v0 - nw : -1;
+            tcol[i] = t >= 0 && t < 16 * NJ && t < N - nw && (((int)t >> 2) & 3) == (lane >> 4) ? (int)t : -1;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             __builtin_amdgcn_sched_barrier(0);
@@ -557,8 +579,8 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
                     if (edge && nw + j * 16 + nsub + e >= N) v[j][e] = -INFINITY;
                     top = fmaxf(top, v[j][e]);
                 }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
+            top = fmaxf(exchanged<16>(top)[0], exchanged<16>(top)[1]);
+            top = fmaxf(exchanged<32>(top)[0], exchanged<32>(top)[1]);
             top *= alpha;
             const float base = top > -INFINITY ? top : 0.0f;   // (no column, or all minus infinity: the sum is 0, not NaN)
             float sum = 0.0f;
@@ -566,18 +588,15 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][e], alpha, -base));
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
+            sum = exchanged<16>(sum)[0] + exchanged<16>(sum)[1];
+            sum = exchanged<32>(sum)[0] + exchanged<32>(sum)[1];
             if (lane < 16 && m < M) head.part[(size_t)(2 * tn + wn) * M + m] = make_float2(top, sum);
-            // the target's column within this wave, where it is one (few rows of few tiles)
-            const int64_t t = m < M ? head.targets[m] - head.v0 - nw : -1;
-            const bool mine = t >= 0 && t < 16 * NJ && t < N - nw && (((int)t >> 2) & 3) == (lane >> 4);
-            if (__ballot(mine) != 0) {
+            if (__ballot(tcol[i] >= 0) != 0) {   // (few rows of few tiles)
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (mine && (int)t == j * 16 + nsub + e) head.picked[m] = v[j][e] * alpha;
+                        if (tcol[i] == j * 16 + nsub + e) head.picked[m] = v[j][e] * alpha;
             }
         }
         return;
@@ -586,23 +605,19 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
         // gradients of the logits over the row's factor, G[m][n]; rows that are ignored and columns beyond N are zero, so that G can be walked in whole slots as the
         // next product's k
         const int mw = m0 + wm * 128 + 8 * mrow;          // first of this lane's eight rows
-        const int nl = n0 + wn * 128 + 2 * nsub;          // first of its columns nl + 32*j + 0..7
-        float lse2[8], up[8], down[8];
+        const int nl = n0 + wn * 16 * NJ + 2 * nsub;      // first of its columns nl + 32*j + 0..7
+        float4 row[8];   // HeadArgs::rows
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row[i] = head.rows[mw + i < M ? mw + i : M - 1];
         int tcol[8];
-        bool keep[8], whole = n0 + wn * 128 + 128 <= N, hit = false;
+        bool keep[8], whole = n0 + (wn + 1) * 16 * NJ <= N, hit = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int m = mw + i;
-            const int64_t t = m < M ? head.targets[m] : head.ignore;
-            keep[i] = t != head.ignore;
+            const int t = __float_as_int(row[i].w);
+            keep[i] = t != INT_MIN;
             whole = whole && keep[i];
-            const float f = keep[i] ? head.factor[m] : 0.0f, inv = f != 0.0f ? 1.0f / f : 0.0f;
-            const float a = keep[i] ? head.dloss[m] : 0.0f, b = keep[i] && head.dlse != nullptr ? head.dlse[m] : 0.0f;
-            lse2[i] = keep[i] ? head.lse[m] * 1.44269504088896341f : 0.0f;
-            up[i] = (a + b) * inv;
-            down[i] = a * inv;
-            const int64_t c = t - head.v0 - nl;   // 32*j + 0..7: this lane's
-            tcol[i] = keep[i] && c >= 0 && c < 128 && (c & 31) < 8 ? (int)c : -1;
+            const int64_t c = (int64_t)t - head.v0 - nl;   // 32*j + 0..7: this lane's
+            tcol[i] = t >= 0 && c >= 0 && c < 16 * NJ && (c & 31) < 8 ? (int)c : -1;
             hit = hit || tcol[i] >= 0;
         }
         // most waves see neither an ignored row, nor an edge, nor a target
@@ -616,17 +631,17 @@ __device__ __forceinline__ void gemm_tile(const char* __restrict__ A, const char
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
-                    g[i][c] = up[i] * __builtin_amdgcn_exp2f(__builtin_fmaf(acc_read(acc[jj + (c >> 2)][i][c & 3]), alpha, -lse2[i]));
+                    g[i][c] = row[i].y * __builtin_amdgcn_exp2f(__builtin_fmaf(acc_read(acc[jj + (c >> 2)][i][c & 3]), alpha, -row[i].x));
             if (!plain) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
-                        if (tcol[i] == 16 * jj + c) g[i][c] -= down[i];
+                        if (tcol[i] == 16 * jj + c) g[i][c] -= row[i].z;
                         if (!keep[i] || n + c >= N) g[i][c] = 0.0f;
                     }
             }
-            if (n < head.ld_g)
+            if (n < head.g_cols)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (mw + i < M)
@@ -1062,11 +1077,43 @@ int best_tile_cols(int M, int N, int fixed = 1) {
     return 32 * nj;
 }
 
-int gemm_head_tiles_n(int N) { return (N + BN - 1) / BN; }
+namespace {
+int launch_head_part(int kind, int nj, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
+                     hipStream_t stream) {
+    const bool ragged = kind <= HEAD_GRAD && K % 64 != 0;
+    typedef void (*kern_t)(const char*, const char*, uint16_t*, int, int, int, float, int, int, const HeadArgs);
+    static const kern_t kerns[12] = {
+        gemm_head_kernel<8, false, HEAD_STATS>, gemm_head_kernel<4, false, HEAD_STATS>, gemm_head_kernel<8, true, HEAD_STATS>, gemm_head_kernel<4, true, HEAD_STATS>,
+        gemm_head_kernel<8, false, HEAD_GRAD>,  gemm_head_kernel<4, false, HEAD_GRAD>,  gemm_head_kernel<8, true, HEAD_GRAD>,  gemm_head_kernel<4, true, HEAD_GRAD>,
+        gemm_head_kernel<8, false, HEAD_DX>,    gemm_head_kernel<4, false, HEAD_DX>,    gemm_head_kernel<8, false, HEAD_DW>,   gemm_head_kernel<4, false, HEAD_DW>};
+    const kern_t kern = kerns[(kind == HEAD_STATS ? 0 : kind == HEAD_GRAD ? 4 : kind == HEAD_DX ? 8 : 10) + (ragged ? 2 : 0) + (nj == 4 ? 1 : 0)];
+    const int rc = set_max_dynamic_lds((const void*)kern, kLdsBytes);
+    if (rc != ROV_OK) return rc;
+    const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + 32 * nj - 1) / (32 * nj);
+    if (tiles_m * tiles_n > 0x7FFFFFFFLL) return ROV_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
+                       (uint16_t*)C, M, N, K, alpha, (int)tiles_m, (int)tiles_n, head);
+    ROV_LAUNCH_CHECK();
+    return ROV_OK;
+}
+
+// How many of `lines` lines of `across` 256 x 256 tiles each run as such: those in full rounds over the compute units, where the rest, cut
+// into tiles of 256 x 128, fits one round of 0.63 times a round's time (a slot of k 890 against 1410 ns); else all.  (1000 x
+// 50257 x 1024: 788 tiles are four rounds, of which the last has 20 tiles.)
+long long wide_lines(long long lines, long long across) {
+    const long long ncu = device_cu_count(), full = lines * across / ncu * ncu / across;
+    return 2 * across * (lines - full) <= ncu ? full : lines;
+}
+}  // namespace
+
+int gemm_head_parts(int M, int N) {
+    const long long lines = (N + BN - 1) / BN, wide = wide_lines(lines, (M + BM - 1) / BM);
+    return (int)(2 * wide + (wide < lines ? 2 * ((N - wide * BN + 127) / 128) : 0));
+}
 
 int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
                      hipStream_t stream) {
-    const bool kn = kind == HEAD_DX || kind == HEAD_DW, kna = kind == HEAD_DW, ragged = !kn && K % 64 != 0;
+    const bool kn = kind == HEAD_DX || kind == HEAD_DW, kna = kind == HEAD_DW;
     if (A == nullptr || W == nullptr || M <= 0 || N <= 0 || K <= 0 || shares <= 0 || shares > 65535) return ROV_ERR_INVALID;
     if (!aligned(A, 16) || !aligned(W, 16) || head.ld_a % 16 != 0 || head.ld_w % 16 != 0 || (!kn && K % 8 != 0)) return ROV_ERR_INVALID;
     const int64_t slots = ((int64_t)K + 63) / 64;
@@ -1076,18 +1123,32 @@ int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int
     if ((unsigned long long)(kna ? slots * 64 : BM) * head.ld_a + 1024 > 0xFFFFFFFFull ||
         (unsigned long long)(kn ? slots * 64 : BN) * head.ld_w + 1024 > 0xFFFFFFFFull)
         return ROV_ERR_UNSUPPORTED;
-    typedef void (*kern_t)(const char*, const char*, uint16_t*, int, int, int, float, int, int, const HeadArgs);
-    const kern_t kern = kind == HEAD_STATS  ? (ragged ? gemm_head_kernel<8, true, HEAD_STATS> : gemm_head_kernel<8, false, HEAD_STATS>)
-                        : kind == HEAD_GRAD ? (ragged ? gemm_head_kernel<8, true, HEAD_GRAD> : gemm_head_kernel<8, false, HEAD_GRAD>)
-                                            : (kna ? gemm_head_kernel<8, false, HEAD_DW> : gemm_head_kernel<8, false, HEAD_DX>);
-    const int rc = set_max_dynamic_lds((const void*)kern, kLdsBytes);
-    if (rc != ROV_OK) return rc;
     const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
-    if (tiles_m * tiles_n > 0x7FFFFFFFLL) return ROV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
-                       (uint16_t*)C, M, N, K, alpha, (int)tiles_m, (int)tiles_n, head);
-    ROV_LAUNCH_CHECK();
-    return ROV_OK;
+    HeadArgs h = head;
+    if (!kn) {   // columns beyond the full rounds: narrower tiles
+        const int wide = (int)(wide_lines(tiles_n, tiles_m) * BN);
+        if (wide >= N) return launch_head_part(kind, 8, A, W, C, M, N, K, alpha, 1, head, stream);
+        if (wide > 0) {
+            h.g_cols = wide;
+            const int rc = launch_head_part(kind, 8, A, W, C, M, wide, K, alpha, 1, h, stream);
+            if (rc != ROV_OK) return rc;
+        }
+        h.v0 += wide;
+        h.g_cols = head.g_cols - wide;
+        if (h.g != nullptr) h.g += wide;
+        if (h.part != nullptr) h.part += (size_t)(wide / 128) * M;
+        return launch_head_part(kind, 4, A, (const char*)W + (size_t)wide * head.ld_w, C, M, N - wide, K, alpha, 1, h, stream);
+    }
+    const int wide = shares > 1 ? M : (int)(wide_lines(tiles_m, tiles_n) * BM);   // rows
+    if (wide >= M) return launch_head_part(kind, 8, A, W, C, M, N, K, alpha, shares, head, stream);
+    if (wide > 0) {
+        const int rc = launch_head_part(kind, 8, A, W, C, wide, N, K, alpha, 1, head, stream);
+        if (rc != ROV_OK) return rc;
+    }
+    if (h.sum != nullptr) h.sum += (size_t)wide * h.ld_sum;
+    h.factor += h.factor_step * wide;
+    return launch_head_part(kind, 4, (const char*)A + (kna ? (size_t)wide * 2 : (size_t)wide * head.ld_a), W, (uint16_t*)C + (size_t)wide * head.ld_out,
+                            M - wide, N, K, alpha, 1, h, stream);
 }
 
 // Is a sum of at most 128 terms done sooner by the any-shape kernel?  Its 64 x 64 tiles pay per 16 terms; the

@@ -109,10 +109,10 @@ int check_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, const v
                           float scaleC);
 // The products of the loss over the vocabulary (bf16, fp32 accumulation; strides ld_a, ld_w in bytes, multiples of 16), as forms of the
 // 256-row kernel with other epilogues.  A [M,K], W [N,K], K contiguous, K % 8 == 0:
-//   HEAD_STATS  z = A W^T * alpha (logits in units of log 2): per row and half tile (128 columns) maximum and sum of exp2 to
-//               part[2 * gemm_head_tiles_n(N)][M], the target's z to picked[m] (rows whose target is one of the N columns, v0 the first);
-//   HEAD_GRAD   G[m][n] = (exp2(z - lse log2 e) * (dloss + dlse) - [v0 + n == target] * dloss) / factor[m] in bf16 to g [M][ld_g], columns
-//               N .. ld_g (N rounded up to 64) and rows of ignored targets (or with factor 0) zero.
+//   HEAD_STATS  z = A W^T * alpha (logits in units of log 2): per row and half tile (of 256 or 128 columns) maximum and sum of exp2 to
+//               part[gemm_head_parts(M, N)][M], the target's z to picked[m] (rows whose target is one of the N columns, v0 the first);
+//   HEAD_GRAD   G[m][n] = rows[m].y * exp2(z - rows[m].x) - [v0 + n == target] * rows[m].z in bf16 to g [M][ld_g]; rows[m].w: the bits of the
+//               int target, negative for none, INT_MIN for a row of zeros whatever its logits are; columns N .. g_cols (N rounded up to 64) are zero.
 // W [K,N], N contiguous, and A [M,K] with rows of whole slots (64 values, zero beyond K; HEAD_DX) or [K,M] (HEAD_DW): A W or A^T W;
 // `shares` workgroups a tile take a share of k each and write fp32 (add: add to) sum[share][M][ld_sum]; sum == NULL (one share): bf16
 // to C, rows of ld_out (out_wide: rows on 8 bytes), times factor[factor_step * m] * scale.
@@ -122,20 +122,18 @@ struct HeadArgs {
     const int64_t* targets = nullptr;
     float2* part = nullptr;
     float* picked = nullptr;
-    const float* lse = nullptr;
-    const float* dloss = nullptr;
-    const float* dlse = nullptr;
+    const float4* rows = nullptr;
     const float* factor = nullptr;
     int64_t factor_step = 1;
     uint16_t* g = nullptr;
-    int64_t ld_g = 0;
-    int64_t ignore = 0, v0 = 0;
+    int64_t ld_g = 0, g_cols = 0;
+    int64_t v0 = 0;
     float scale = 1.0f;
     float* sum = nullptr;
     int64_t ld_sum = 0, ld_out = 0;
     bool add = false, out_wide = false;
 };
-int gemm_head_tiles_n(int N);
+int gemm_head_parts(int M, int N);
 int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
                      hipStream_t stream);
 

@@ -15,6 +15,7 @@
 // which changes nothing where they are all the same, and dW by the largest.
 // fp32: the fp32 products of gemm_ring.hip; a piece's logits live in the workspace while they are reduced, or turned into G in place.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -117,9 +118,10 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(float* __restrict__ z, f
 
 // ------------------------------------------------------------------ bf16
 // factor[m]: dloss, or dloss + dlse where dloss is next to nothing beside it; 0 for rows of ignored targets, NaN for targets outside the
-// vocabulary.  factor[M]: the largest of their magnitudes.  One workgroup.
+// vocabulary.  factor[M]: the largest of their magnitudes.  rows: what the epilogue for G needs of a row.  One workgroup.
 __global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t* __restrict__ targets, int64_t ignore, int V, const float* __restrict__ dloss,
-                                                           const float* __restrict__ dlse, float* __restrict__ factor, int M) {
+                                                           const float* __restrict__ dlse, const float* __restrict__ lse,
+                                                           float* __restrict__ factor, float4* __restrict__ rows, int M) {
     __shared__ float red[16];
     float most = 0.0f;
     for (int m = threadIdx.x; m < M; m += 1024) {
@@ -127,6 +129,9 @@ __global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t* __rest
         const float a = dloss[m], s = dlse != nullptr ? a + dlse[m] : a;
         const float f = t == ignore ? 0.0f : !in_vocab(t, V) ? NAN : fabsf(a) * 1048576.0f >= fabsf(s) ? a : s;
         factor[m] = f;
+        const bool keep = t != ignore && f != 0.0f;
+        rows[m] = make_float4(keep ? lse[m] * 1.44269504088896341f : 0.0f, keep ? s / f : 0.0f, keep ? a / f : 0.0f,
+                              __int_as_float(!keep ? INT_MIN : in_vocab(t, V) ? (int)t : -1));
         most = fmaxf(most, fabsf(f));
     }
 #pragma unroll
@@ -402,7 +407,7 @@ int shares_of(int M, int N, int64_t K) {
 struct HeadLayout {
     int piece, packed, shares_x, shares_w;   // columns of a piece, of a piece of W that is packed
     int64_t kp, ks;                          // K as rows of packed operands, of sums
-    size_t x, w, part, picked, factor, xs, g, sum_x, sum_w, total;   // xs: X times its rows' factors
+    size_t x, w, part, picked, factor, rows, xs, g, sum_x, sum_w, total;   // xs: X times its rows' factors
 };
 HeadLayout head_layout(int M, int V, int K, int asked, bool backward) {
     HeadLayout l{};
@@ -418,12 +423,16 @@ HeadLayout head_layout(int M, int V, int K, int asked, bool backward) {
     l.x = take((size_t)M * l.kp * 2);
     l.w = take((size_t)l.packed * l.kp * 2);
     if (!backward) {
-        l.part = take((size_t)2 * gemm_head_tiles_n(V) * M * sizeof(float2));
+        // (whole, or in packed pieces: as many partial statistics, up to the narrower tiles of each)
+        const int64_t whole = gemm_head_parts(M, V), by_piece = (int64_t)(V / l.packed) * gemm_head_parts(M, l.packed) +
+                                                               (V % l.packed != 0 ? gemm_head_parts(M, V % l.packed) : 0);
+        l.part = take((size_t)(whole > by_piece ? whole : by_piece) * M * sizeof(float2));
         l.picked = take((size_t)M * 4);
     } else {
         l.shares_x = shares_of(M, K, l.packed);
         l.shares_w = shares_of(l.packed, K, M);
         l.factor = take(((size_t)M + 1) * 4);
+        l.rows = take((size_t)M * sizeof(float4));
         l.xs = take((size_t)M * l.kp * 2);
         l.g = take((size_t)M * up_to(l.piece, 64) * 2);
         l.sum_x = take(l.shares_x > 1 || l.packed < V ? (size_t)l.shares_x * M * l.ks * 4 : 0);
@@ -529,7 +538,9 @@ int head_forward(const void* X, const void* W, const int64_t* targets, int M, in
         const int rc = pack(X, ldx, ws + l.x, M, K, l.kp, nullptr, st);
         if (rc != ROV_OK) return rc;
     }
+    int count = 0;
     if (fit_w) {
+        count = gemm_head_parts(M, V);
         h.ld_w = (size_t)ldw * 2;
         const int rc = launch_gemm_head(HEAD_STATS, x, W, nullptr, M, V, kx, scale * kLog2e, 1, h, st);
         if (rc != ROV_OK) return rc;
@@ -540,18 +551,19 @@ int head_forward(const void* X, const void* W, const int64_t* targets, int M, in
             int rc = pack((const char*)W + (size_t)v0 * ldw * 2, ldw, ws + l.w, cols, K, l.kp, nullptr, st);
             if (rc != ROV_OK) return rc;
             h.v0 = v0;
-            h.part = (float2*)(ws + l.part) + (size_t)(v0 / 128) * M;   // (pieces are whole tiles)
+            h.part = (float2*)(ws + l.part) + (size_t)count * M;
+            count += gemm_head_parts(M, cols);
             rc = launch_gemm_head(HEAD_STATS, x, ws + l.w, nullptr, M, cols, kx, scale * kLog2e, 1, h, st);
             if (rc != ROV_OK) return rc;
         }
     }
     // (few rows: more threads a row, 16 x 131072 12 -> 5 us)
     if (M < 1024)
-        hipLaunchKernelGGL(xent_join_kernel<4>, dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, (const float2*)(ws + l.part), 2 * gemm_head_tiles_n(V),
+        hipLaunchKernelGGL(xent_join_kernel<4>, dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, (const float2*)(ws + l.part), count,
                            h.picked, M, V, targets, ignore, loss, lse);
     else
         hipLaunchKernelGGL(xent_join_kernel<16>, dim3((unsigned)((M + 15) / 16)), dim3(256), 0, st, (const float2*)(ws + l.part),
-                           2 * gemm_head_tiles_n(V), h.picked, M, V, targets, ignore, loss, lse);
+                           count, h.picked, M, V, targets, ignore, loss, lse);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
@@ -560,13 +572,10 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
                   int64_t ldx, int64_t ldw, float scale, int64_t ignore, void* dX, void* dW, int64_t lddx, int64_t lddw, char* ws, const HeadLayout& l,
                   hipStream_t st) {
     HeadArgs h;
-    h.targets = targets;
-    h.lse = lse;
-    h.dloss = dloss;
-    h.dlse = dlse;
-    h.ignore = ignore;
+    h.rows = (const float4*)(ws + l.rows);
     h.factor = (const float*)(ws + l.factor);
-    hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, ignore, V, dloss, dlse, (float*)(ws + l.factor), M);
+    hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, ignore, V, dloss, dlse, lse,
+                       (float*)(ws + l.factor), (float4*)(ws + l.rows), M);
     ROV_LAUNCH_CHECK();
     const bool fit_w = rows_fit(W, ldw, K);
     const char* x = (const char*)X;
@@ -599,7 +608,7 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
         h.ld_w = (size_t)ld * 2;
         h.v0 = v0;
         h.g = (uint16_t*)(ws + l.g);
-        h.ld_g = ldg;
+        h.ld_g = h.g_cols = ldg;
         rc = launch_gemm_head(HEAD_GRAD, x, w, nullptr, M, cols, kx, scale * kLog2e, 1, h, st);
         if (rc != ROV_OK) return rc;
         if (dX != nullptr) {

@@ -66,7 +66,9 @@ def close(got, want, tol, what):
 
 
 SIZES = [(1, 1, 1, 0), (1, 300, 8, 0), (3, 5, 7, 0), (17, 1000, 64, 0), (64, 257, 128, 0), (130, 2050, 96, 512), (257, 999, 130, 256), (300, 1300, 264, 0),
-         (33, 5003, 513, 1024), (512, 4096, 512, 0), (513, 2049, 1000, 700), (1025, 777, 72, 0), (2, 70001, 40, 0)]
+         (33, 5003, 513, 1024), (512, 4096, 512, 0), (513, 2049, 1000, 700), (1025, 777, 72, 0), (2, 70001, 40, 0),
+         # more than a round of 256 x 256 tiles and a rest in narrower ones: columns, columns of packed operands, rows of dX
+         (300, 70001, 64, 0), (300, 40001, 33, 0), (66000, 300, 16, 0)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
