@@ -34,6 +34,18 @@ struct NormParams {
     float x_scale, h_scale, eps, inv_n, yn_inv;   // yn_inv: 1 / (scale of the e4m3 result)
 };
 
+// W consecutive fp32 values, 16 bytes at a time where there are four
+template <int W>
+__device__ __forceinline__ void store_floats(float* to, const float (&v)[W]) {
+    if constexpr (W % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < W; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j) to[j] = v[j];
+    }
+}
+
 template <typename T, int W>
 __device__ __forceinline__ void load_or(const void* base, int at, float (&f)[W], float otherwise) {
     if (base != nullptr) {
@@ -302,11 +314,11 @@ __global__ __launch_bounds__(NT, VPT * W <= 8 ? 4 : 1) void norm_bwd_kernel(cons
     for (int c = 0; c < VPT; ++c) {
         const int e = (c * NT + (int)threadIdx.x) * W;
         if (e >= p.n) continue;
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            if (p.part_h != nullptr) p.part_h[(int64_t)blockIdx.x * p.n + e + j] = WHOLE ? col_g[c][j] : col_h[c][j];
-            if (p.part_y != nullptr) p.part_y[(int64_t)blockIdx.x * p.n + e + j] = col_y[c][j];
+        if (p.part_h != nullptr) {
+            if constexpr (WHOLE) store_floats<W>(p.part_h + (int64_t)blockIdx.x * p.n + e, col_g[c]);
+            else store_floats<W>(p.part_h + (int64_t)blockIdx.x * p.n + e, col_h[c]);
         }
+        if (p.part_y != nullptr) store_floats<W>(p.part_y + (int64_t)blockIdx.x * p.n + e, col_y[c]);
     }
 }
 
@@ -388,9 +400,9 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const NormSumParams p) {
 struct RowShape { int nt, vpt; };
 RowShape row_shape(int pieces, int w) {
     if (pieces <= 64) return {64, 1};
+    if (w == 1 && pieces <= 1024) return {pieces <= 256 ? 64 : pieces <= 512 ? 128 : 256, 4};
     if (pieces <= 128) return {128, 1};
     if (pieces <= 256) return {256, 1};
-    if (w == 1 && pieces <= 1024) return {256, 4};
     if (pieces <= 512) return {512, 1};
     if (pieces <= 1024) return {1024, 1};
     if (pieces <= 4096) return {1024, 4};
@@ -402,15 +414,17 @@ void launch_fwd(const NormParams& p, hipStream_t stream) {
     const RowShape s = row_shape((p.n + W - 1) / W, W);
     const dim3 grid((unsigned)p.rows);
 #define ROV_FWD(NT, VPT) hipLaunchKernelGGL((norm_fwd_kernel<T, W, NT, VPT, OUT8>), grid, dim3(NT), 0, stream, p)
-    if (s.nt == 64) ROV_FWD(64, 1);
-    else if (s.nt == 128) ROV_FWD(128, 1);
-    else if (s.nt == 256 && s.vpt == 1) ROV_FWD(256, 1);
+    if (s.nt == 64 && s.vpt == 1) ROV_FWD(64, 1);
     else if constexpr (W == 1) {
-        if (s.nt == 256) ROV_FWD(256, 4);
+        if (s.nt == 64) ROV_FWD(64, 4);
+        else if (s.nt == 128) ROV_FWD(128, 4);
+        else if (s.nt == 256) ROV_FWD(256, 4);
         else if (s.vpt == 4) ROV_FWD(1024, 4);
         else ROV_FWD(1024, 32);
     } else {
-        if (s.nt == 512) ROV_FWD(512, 1);
+        if (s.nt == 128) ROV_FWD(128, 1);
+        else if (s.nt == 256) ROV_FWD(256, 1);
+        else if (s.nt == 512) ROV_FWD(512, 1);
         else if (s.vpt == 1) ROV_FWD(1024, 1);
         else if (W == 8 || s.vpt == 4) ROV_FWD(1024, 4);
         else if constexpr (W == 4) ROV_FWD(1024, 8);
@@ -423,15 +437,17 @@ void launch_bwd(const NormBwdParams& p, int blocks, hipStream_t stream) {
     const RowShape s = row_shape((p.n + W - 1) / W, W);
     const dim3 grid((unsigned)blocks);
 #define ROV_BWD(NT, VPT) hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, VPT, WHOLE>), grid, dim3(NT), 0, stream, p)
-    if (s.nt == 64) ROV_BWD(64, 1);
-    else if (s.nt == 128) ROV_BWD(128, 1);
-    else if (s.nt == 256 && s.vpt == 1) ROV_BWD(256, 1);
+    if (s.nt == 64 && s.vpt == 1) ROV_BWD(64, 1);
     else if constexpr (W == 1) {
-        if (s.nt == 256) ROV_BWD(256, 4);
+        if (s.nt == 64) ROV_BWD(64, 4);
+        else if (s.nt == 128) ROV_BWD(128, 4);
+        else if (s.nt == 256) ROV_BWD(256, 4);
         else if (s.vpt == 4) ROV_BWD(1024, 4);
         else ROV_BWD(1024, 32);
     } else {
-        if (s.nt == 512) ROV_BWD(512, 1);
+        if (s.nt == 128) ROV_BWD(128, 1);
+        else if (s.nt == 256) ROV_BWD(256, 1);
+        else if (s.nt == 512) ROV_BWD(512, 1);
         else if (s.vpt == 1) ROV_BWD(1024, 1);
         else if (W == 8 || s.vpt == 4) ROV_BWD(1024, 4);
         else if constexpr (W == 4) ROV_BWD(1024, 8);
