@@ -578,7 +578,7 @@ int rov_rope(const rov_rope_cfg *cfg, const void *Q, void *Qo, const void *K, vo
  * row r uses gate row r / rows_per_gate; weights [n].  All of dtype ROV_F32 or ROV_BF16, arithmetic and sums in fp32; yn
  * is formed from y before y is rounded.  yn_fp8_scale > 0 (bf16 only): yn holds OCP e4m3 bytes of
  * (value / yn_fp8_scale), as the fp8 products take their activations; else 0.
- * ld: row strides of x, h, y, yn in elements (>= n).  y and yn may be x or h (with the same stride).
+ * ld: row strides of x, h, y, yn in elements (>= n).  y and yn may be x or h (with the same stride; e4m3 yn may not), not each other.
  * n > 32768: ROV_ERR_UNSUPPORTED. */
 int rov_norm_residual(const void *x, const void *h, const void *w_post, const void *gate, const void *w_pre,
                       void *y, void *yn, int64_t rows, int n, const int64_t ld[4], int64_t rows_per_gate, int dtype,
@@ -587,7 +587,7 @@ int rov_norm_residual(const void *x, const void *h, const void *w_post, const vo
 /* Its gradients.  y: the forward pass's result, h its input; dy, dn: the gradients that reach y (from the residual
  * stream; NULL: none) and yn (NULL exactly when w_pre is).  dx, dh [rows, n] in dtype; dw_post [n], dgate
  * [rows / rows_per_gate, n] and dw_pre [n] in fp32, summed in a fixed order.  Results that are NULL are not made; h may
- * be NULL where neither w_post nor dgate needs it, y without w_pre.  dx and dh may be any of the four inputs (same stride).
+ * be NULL where neither w_post nor dgate needs it, y without w_pre.  dx and dh may be any of the four inputs (same stride), not each other.
  * ld: row strides of y, h, dy, dn, dx, dh.  workspace: 16-byte aligned device scratch of
  * rov_norm_residual_bwd_workspace_bytes (0 for invalid arguments), needed for the three sums only. */
 size_t rov_norm_residual_bwd_workspace_bytes(int64_t rows, int n, int64_t rows_per_gate, int dtype);
@@ -631,7 +631,9 @@ int rov_block_forward_opts(const rov_block_weights *w, const rov_block_opts *opt
  * scale > 0.  dtype of X and W: ROV_F32 or ROV_BF16; row strides ldx, ldw >= K in elements.  Logits and sums are fp32.
  * vocab_piece: columns of a piece (rounded up to 256), 0: chosen by the library; it sets the workspace's size and
  * does not change what is computed beyond the order of fp32 sums.
- * workspace: 256-byte aligned device scratch of rov_linear_xent_workspace_bytes (0 for invalid arguments). */
+ * workspace: 256-byte aligned device scratch of rov_linear_xent_workspace_bytes (0 for invalid arguments).
+ * bf16 operands are reached by 32-bit offsets: 256 rows of X or W, and for the gradients M rows of K or of a piece, must stay below
+ * 4 GiB, else ROV_ERR_UNSUPPORTED. */
 size_t rov_linear_xent_workspace_bytes(int M, int V, int K, int dtype, int backward, int vocab_piece);
 int rov_linear_xent(const void *X, const void *W, const int64_t *targets, int M, int V, int K, int64_t ldx,
                     int64_t ldw, int dtype, float scale, int64_t ignore_index, float *loss, float *lse,

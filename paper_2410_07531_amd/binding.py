@@ -718,6 +718,8 @@ def norm_residual(x, h, w_pre=None, w_post=None, gate=None, x_scale=1.0, h_scale
     """(y, yn): y = x_scale * x + h_scale * gate * (RMS(h) * w_post), yn = RMS(y) * w_pre (None without w_pre); x, h [..., n],
     gate [n] or [gates, n] (consecutive rows share a gate).  yn_fp8_scale: yn in e4m3 bytes with that scale."""
     shape = x.shape
+    if x.numel() == 0 or x.dim() == 0:
+        raise ValueError("norm_residual: x must be [..., n], not empty")
     n = shape[-1]
     _on_gpu("norm_residual", x.dtype, ("x", "h", "w_pre", "w_post", "gate", "y"), (x, h, w_pre, w_post, gate, y))
     if y is None:
@@ -747,6 +749,8 @@ def norm_residual_bwd(y, h, dy, dn=None, w_pre=None, w_post=None, gate=None, x_s
     if like is None:
         raise ValueError("norm_residual_bwd: dy or dn is needed")
     shape, dt = like.shape, like.dtype
+    if like.numel() == 0 or like.dim() == 0:
+        raise ValueError("norm_residual_bwd: the gradients must be [..., n], not empty")
     n = shape[-1]
     names, tensors = ("y", "h", "dy", "dn", "dx", "dh"), (y, h, dy, dn, dx, dh)
     _on_gpu("norm_residual_bwd", dt, names + ("w_pre", "w_post", "gate"), tensors + (w_pre, w_post, gate))

@@ -498,6 +498,13 @@ int check_norm_residual(const void* x, const void* h, const void* w_post, const 
         if (!aligned(q, esz)) return ROV_ERR_INVALID;
     for (int i = 0; i < (w_pre != nullptr ? 4 : 3); ++i)
         if (ld[i] < n && rows > 1) return ROV_ERR_INVALID;
+    // in place is element by element: the same stride and type, and one result a buffer
+    if (y == yn || (out8 && (yn == x || yn == h))) return ROV_ERR_INVALID;
+    const void* const ins[2] = {x, h};
+    const void* const outs[2] = {y, yn};
+    for (int i = 0; i < 2; ++i)
+        for (int o = 0; o < 2; ++o)
+            if (outs[o] == ins[i] && ld[2 + o] != ld[i] && rows > 1) return ROV_ERR_INVALID;
     return ROV_OK;
 }
 
@@ -563,6 +570,10 @@ extern "C" int rov_norm_residual_bwd(const void* y, const void* h, const void* w
         if (tensors[i] != nullptr && rows > 1 && ld[i] < n) return ROV_ERR_INVALID;
     }
     if (!aligned(dw_post, 4) || !aligned(dgate, 4) || !aligned(dw_pre, 4)) return ROV_ERR_INVALID;
+    if (dx != nullptr && dx == dh) return ROV_ERR_INVALID;
+    for (int o = 4; o < 6; ++o)   // in place: the same stride
+        for (int i = 0; i < 4; ++i)
+            if (tensors[o] != nullptr && tensors[o] == tensors[i] && ld[o] != ld[i] && rows > 1) return ROV_ERR_INVALID;
     if (rc != ROV_OK) return rc;
     const int w = dtype == ROV_F32 ? 4 : 8;
     bool vec = n % w == 0;

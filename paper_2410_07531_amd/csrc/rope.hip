@@ -194,13 +194,14 @@ int check_rope_cfg(const rov_rope_cfg* c, int d) {
 }
 
 int check_rope(const rov_rope_cfg* c, const void* Q, const void* Qo, const void* K, const void* Ko, int B, int S, int H, int Hkv,
-               int d, const int64_t strides[12], int dtype) {
+               int d, const int64_t strides[12], int dtype, const int64_t* positions) {
     const int rc = check_rope_cfg(c, d);
     if (rc != ROV_OK && rc != ROV_ERR_UNSUPPORTED) return rc;
     if (Q == nullptr || Qo == nullptr || strides == nullptr || B <= 0 || S <= 0 || H <= 0 || Hkv < 0) return ROV_ERR_INVALID;
     if (Hkv > 0 && (K == nullptr || Ko == nullptr)) return ROV_ERR_INVALID;
     if (dtype != ROV_F32 && dtype != ROV_BF16) return dtype == ROV_FP8_E4M3 ? ROV_ERR_UNSUPPORTED : ROV_ERR_INVALID;
     const size_t esz = dtype == ROV_F32 ? 4 : 2;
+    if (!aligned(positions, 8)) return ROV_ERR_INVALID;
     if (!aligned(Q, esz) || !aligned(Qo, esz) || (Hkv > 0 && (!aligned(K, esz) || !aligned(Ko, esz)))) return ROV_ERR_INVALID;
     // a buffer turned in place is its own result, stride for stride
     for (int t = 0; t < (Hkv > 0 ? 2 : 1); ++t)
@@ -215,7 +216,7 @@ int launch_rope_cfg(const rov_rope_cfg* c, const void* Q, void* Qo, const void* 
                     const int64_t strides[12], int dtype, const int64_t* positions, int64_t positions_stride, int backward,
                     hipStream_t stream) {
     {
-        const int rc = check_rope(c, Q, Qo, K, Ko, B, S, H, Hkv, d, strides, dtype);
+        const int rc = check_rope(c, Q, Qo, K, Ko, B, S, H, Hkv, d, strides, dtype, positions);
         if (rc != ROV_OK) return rc;
     }
     RopeParams p{};

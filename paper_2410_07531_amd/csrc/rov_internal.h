@@ -163,7 +163,7 @@ int launch_rmsnorm_fp8(const void* x, const void* weight, void* y8, int64_t rows
                        hipStream_t stream);
 // rope.hip, norm.hip: see rov_rope and rov_norm_residual
 int check_rope(const rov_rope_cfg* c, const void* Q, const void* Qo, const void* K, const void* Ko, int B, int S, int H, int Hkv, int d,
-               const int64_t strides[12], int dtype);
+               const int64_t strides[12], int dtype, const int64_t* positions);
 int launch_rope_cfg(const rov_rope_cfg* c, const void* Q, void* Qo, const void* K, void* Ko, int B, int S, int H, int Hkv, int d,
                     const int64_t strides[12], int dtype, const int64_t* positions, int64_t positions_stride, int backward, hipStream_t stream);
 int check_norm_residual(const void* x, const void* h, const void* w_post, const void* gate, const void* w_pre, const void* y, const void* yn,

@@ -663,7 +663,8 @@ int block_forward_impl(const rov_block_weights* w, const rov_block_opts* opts, c
         ROV_STEP(check_gemm_swiglu(h, w->wg, w->wu, u, (int)T, ffn, hidden));
     ROV_STEP(check_gemm(u, w->wd, y, around ? nullptr : x2, EPI_ADD, (int)T, hidden, ffn, dt, 1));
     if (rope != nullptr)
-        ROV_STEP(check_rope(rope, qkv, qkv, (char*)qkv + (size_t)H * d * 2, (char*)qkv + (size_t)H * d * 2, B, S, H, Hkv, d, rope_strides, ROV_BF16));
+        ROV_STEP(check_rope(rope, qkv, qkv, (char*)qkv + (size_t)H * d * 2, (char*)qkv + (size_t)H * d * 2, B, S, H, Hkv, d, rope_strides, ROV_BF16,
+                            opts->positions));
     if (around) {
         ROV_STEP(check_norm_residual(x, x2, opts->post1, opts->gate1, w->norm2, x2, h, T, hidden, lds, per_gate, ROV_BF16, opts->x_scale, opts->h_scale,
                                      cfg->eps, f8 ? sa2 : 0.0f));

@@ -383,10 +383,14 @@ XentLayout layout(int M, int V, int K, int asked, bool backward) {
     return l;
 }
 
-// Columns of a piece of the bf16 backward pass: G takes at most 256 MiB.  Columns of W packed at a time, where it has to be: 128 MiB.
-int piece_cols_bf16(int M, int V, int asked) {
+constexpr int64_t kPanel = ((int64_t)1 << 32) - (1 << 20);   // bytes that an operand's 32-bit offsets reach, with room for a slot
+
+// Columns of a piece of the bf16 backward pass: G takes at most 256 MiB, and W's rows stay within reach.  Columns of W packed at a time, where it has to be: 128 MiB.
+int piece_cols_bf16(int M, int V, int64_t kp, int asked) {
     int64_t p = asked > 0 ? up_to(asked, 256) : ((int64_t)128 << 20) / M / 256 * 256;
     if (asked <= 0 && p < 1024) p = 1024;
+    const int64_t reach = kPanel / (2 * kp) / 256 * 256;
+    if (p > reach && reach > 0) p = reach;
     return p > V ? V : (int)p;
 }
 int pack_cols(int V, int64_t kp) {
@@ -417,7 +421,7 @@ HeadLayout head_layout(int M, int V, int K, int asked, bool backward) {
     auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
     l.packed = pack_cols(V, l.kp);
     if (backward) {
-        l.piece = piece_cols_bf16(M, V, asked);
+        l.piece = piece_cols_bf16(M, V, l.kp, asked);
         if (l.packed > l.piece) l.packed = l.piece;
     }
     l.x = take((size_t)M * l.kp * 2);
@@ -511,12 +515,12 @@ int outer(const void* G, int64_t ldg, const void* X, int64_t ldx, uint16_t* out,
 bool rows_fit(const void* p, int64_t ld, int K) { return K % 8 == 0 && ld % 8 == 0 && aligned(p, 16); }
 constexpr float kLog2e = 1.44269504088896341f;
 
-// Operands are addressed with 32-bit byte offsets: 256 rows, or all rows of k of the products for dX (a piece of W) and dW (X, G).
-int check_head(int M, int K, int64_t ldx, int64_t ldw, const HeadLayout& l, bool backward) {
-    const int64_t most = ((int64_t)1 << 32) - 1024;
+// Operands are addressed with 32-bit byte offsets: 256 rows, or all rows of k of the products for dX (a piece of W, packed where its
+// own rows reach too far) and dW (X times its factors, G).
+int check_head(int M, int64_t ldx, int64_t ldw, const HeadLayout& l, bool backward) {
     const int64_t ld = ldx > ldw ? ldx : ldw;
-    if (512 * up_to(ld, 8) > most) return ROV_ERR_UNSUPPORTED;
-    if (backward && (up_to(l.piece, 64) * 2 * up_to(ldw, 8) > most || up_to(M, 64) * 2 * l.kp > most || up_to(M, 64) * 2 * up_to(l.piece, 64) > most))
+    if (512 * up_to(ld, 8) > kPanel || 512 * l.kp > kPanel) return ROV_ERR_UNSUPPORTED;
+    if (backward && (up_to(l.packed, 64) * 2 * l.kp > kPanel || up_to(M, 64) * 2 * l.kp > kPanel || up_to(M, 64) * 2 * up_to(l.piece, 64) > kPanel))
         return ROV_ERR_UNSUPPORTED;
     return ROV_OK;
 }
@@ -577,7 +581,7 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
     hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, ignore, V, dloss, dlse, lse,
                        (float*)(ws + l.factor), (float4*)(ws + l.rows), M);
     ROV_LAUNCH_CHECK();
-    const bool fit_w = rows_fit(W, ldw, K);
+    const bool fit_w = rows_fit(W, ldw, K) && up_to(l.piece, 64) * 2 * ldw <= kPanel;
     const char* x = (const char*)X;
     h.ld_a = (size_t)ldx * 2;
     int rc = ROV_OK;
@@ -663,7 +667,7 @@ extern "C" int rov_linear_xent(const void* X, const void* W, const int64_t* targ
     if (workspace == nullptr || !aligned(workspace, kAlign)) return ROV_ERR_INVALID;
     if (dtype == ROV_BF16) {
         const HeadLayout hl = head_layout(M, V, K, vocab_piece, false);
-        ROV_STEP(check_head(M, K, ldx, ldw, hl, false));
+        ROV_STEP(check_head(M, ldx, ldw, hl, false));
         if (workspace_bytes < hl.total) return ROV_ERR_WORKSPACE;
         return head_forward(X, W, targets, M, V, K, ldx, ldw, scale, ignore_index, loss, lse, (char*)workspace, hl, (hipStream_t)stream);
     }
@@ -703,7 +707,7 @@ extern "C" int rov_linear_xent_bwd(const void* X, const void* W, const int64_t* 
     if (workspace == nullptr || !aligned(workspace, kAlign)) return ROV_ERR_INVALID;
     if (dtype == ROV_BF16) {
         const HeadLayout hl = head_layout(M, V, K, vocab_piece, true);
-        ROV_STEP(check_head(M, K, ldx, ldw, hl, true));
+        ROV_STEP(check_head(M, ldx, ldw, hl, true));
         if (workspace_bytes < hl.total) return ROV_ERR_WORKSPACE;
         return head_backward(X, W, targets, lse, dloss, dlse, M, V, K, ldx, ldw, scale, ignore_index, dX, dW, lddx, lddw, (char*)workspace, hl,
                              (hipStream_t)stream);

@@ -137,6 +137,23 @@ def test_strided_operands_and_surroundings(dtype):
             assert bool((w[:, :pad] == 5.0).all()) and bool((w[:, pad + K:] == 5.0).all())
 
 
+def test_rows_of_w_that_reach_beyond_4_gib():
+    # 640 rows, 8 MiB apart: the gradients' products take packed pieces instead
+    M, V, K = 40, 600, 64
+    X, W, t, dloss, _ = make(M, V, K, "bf16", seed=10)
+    far = torch.empty(V * 2 ** 22, dtype=torch.bfloat16, device="cuda").view(V, 2 ** 22)[:, 8:8 + K]
+    far.copy_(W)
+    r = reference(X, W, t, dloss)
+    loss, lse = rov.linear_xent(X, far, t)
+    close(loss, r["loss"], r["tol"], "loss")
+    dX, dW = rov.linear_xent_bwd(X, far, t, lse, dloss)
+    close(dX, r["dX"], r["tX"], "dX")
+    close(dW, r["dW"], r["tW"], "dW")
+    with pytest.raises(rov.RovError) as e:      # 256 rows of X beyond 4 GiB
+        rov.linear_xent(torch.empty(2 ** 24 + 64, dtype=torch.bfloat16, device="cuda").as_strided((2, K), (2 ** 24, 1)), W, t[:2])
+    assert e.value.code == rov.ERR_UNSUPPORTED
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ignored_rows_may_hold_anything(dtype):
     # padding: NaN and infinity in the hidden states and in the gradients of ignored rows reach nothing

@@ -255,6 +255,11 @@ def test_refusals_in_the_binding():
             rov.norm_residual(x, **bad)
     with pytest.raises(TypeError):
         rov.norm_residual(x, x.to(torch.bfloat16))
+    for empty in (torch.zeros(0, 64, device="cuda"), torch.zeros(4, 0, device="cuda"), torch.zeros((), device="cuda")):
+        with pytest.raises(ValueError):
+            rov.norm_residual(empty, empty)
+        with pytest.raises(ValueError):
+            rov.norm_residual_bwd(empty, empty, empty)
     with pytest.raises(ValueError):
         rov.norm_residual_bwd(x, x, None)
     with pytest.raises(rov.RovError):

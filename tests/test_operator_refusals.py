@@ -12,10 +12,10 @@ P = 4096     # "pointers"
 INVALID, UNSUPPORTED, WORKSPACE = rov.ERR_INVALID, rov.ERR_UNSUPPORTED, rov.ERR_WORKSPACE
 
 
-def _rope(cfg=None, Q=P, Qo=2 * P, K=3 * P, Ko=4 * P, B=1, S=4, H=2, Hkv=1, d=64, strides=None, dtype=rov.BF16, **c):
+def _rope(cfg=None, Q=P, Qo=2 * P, K=3 * P, Ko=4 * P, B=1, S=4, H=2, Hkv=1, d=64, strides=None, dtype=rov.BF16, positions=None, **c):
     cfg = rov.make_rope_cfg(**{"rot": 64, "theta": 1e4, **c}) if cfg is None else cfg
     st = [S * H * d, H * d, d] * 2 + [S * Hkv * d, Hkv * d, d] * 2 if strides is None else strides
-    return rov.load().rov_rope(ctypes.byref(cfg), Q, Qo, K, Ko, B, S, H, Hkv, d, (ctypes.c_int64 * 12)(*st), dtype, None, 0, 0, None)
+    return rov.load().rov_rope(ctypes.byref(cfg), Q, Qo, K, Ko, B, S, H, Hkv, d, (ctypes.c_int64 * 12)(*st), dtype, positions, 0, 0, None)
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -25,13 +25,13 @@ def _rope(cfg=None, Q=P, Qo=2 * P, K=3 * P, Ko=4 * P, B=1, S=4, H=2, Hkv=1, d=64
     (dict(scaling=rov.ROPE_SCALE_LINEAR, factor=0.0), INVALID), (dict(scaling=rov.ROPE_SCALE_PARTS, factor=8.0), INVALID),   # no trained length
     (dict(scaling=rov.ROPE_SCALE_PARTS, factor=8.0, trained_len=8, turns_low=4.0, turns_high=4.0), INVALID),
     (dict(magnitude=float("nan")), INVALID), (dict(dtype=7), INVALID), (dict(dtype=rov.FP8_E4M3), UNSUPPORTED), (dict(d=520, rot=64), UNSUPPORTED),
-    (dict(Q=P + 1), INVALID), (dict(Qo=P, strides=[512, 128, 64, 512, 128, 32] + [256, 64, 64] * 2), INVALID),   # in place, other strides
+    (dict(Q=P + 1), INVALID), (dict(positions=P + 4), INVALID), (dict(Qo=P, strides=[512, 128, 64, 512, 128, 32] + [256, 64, 64] * 2), INVALID),   # in place, other strides
 ])
 def test_rope_refuses(kw, code):
     assert _rope(**kw) == code
 
 
-def _norm(x=P, h=P, w_post=P, gate=P, w_pre=P, y=P, yn=P, rows=8, n=64, ld=(64, 64, 64, 64), per=4, dtype=rov.BF16, xs=1.0, hs=1.0, eps=1e-5, fp8=0.0):
+def _norm(x=P, h=2 * P, w_post=P, gate=P, w_pre=P, y=3 * P, yn=4 * P, rows=8, n=64, ld=(64, 64, 64, 64), per=4, dtype=rov.BF16, xs=1.0, hs=1.0, eps=1e-5, fp8=0.0):
     return rov.load().rov_norm_residual(x, h, w_post, gate, w_pre, y, yn, rows, n, (ctypes.c_int64 * 4)(*ld), per, dtype, xs, hs, eps, fp8, None)
 
 
@@ -40,12 +40,13 @@ def _norm(x=P, h=P, w_post=P, gate=P, w_pre=P, y=P, yn=P, rows=8, n=64, ld=(64, 
     (dict(n=0), INVALID), (dict(per=3), INVALID), (dict(per=0), INVALID), (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID),
     (dict(xs=float("inf")), INVALID), (dict(dtype=9), INVALID), (dict(dtype=rov.FP8_E4M3), UNSUPPORTED), (dict(n=40000, ld=(40000,) * 4), UNSUPPORTED),
     (dict(ld=(64, 63, 64, 64)), INVALID), (dict(fp8=-1.0), INVALID), (dict(fp8=1.0, dtype=rov.F32), UNSUPPORTED), (dict(x=P + 1), INVALID),
+    (dict(yn=3 * P), INVALID), (dict(fp8=1.0, yn=P), INVALID), (dict(y=P, ld=(64, 64, 72, 64)), INVALID), (dict(yn=2 * P, ld=(64, 72, 64, 64)), INVALID),
 ])
 def test_norm_residual_refuses(kw, code):
     assert _norm(**kw) == code
 
 
-def _norm_bwd(y=P, h=P, w_post=P, gate=P, w_pre=P, dy=P, dn=P, dx=P, dh=P, dw_post=P, dgate=P, dw_pre=P, rows=8, n=64, ld=(64,) * 6, per=4,
+def _norm_bwd(y=P, h=2 * P, w_post=P, gate=P, w_pre=P, dy=3 * P, dn=4 * P, dx=5 * P, dh=6 * P, dw_post=P, dgate=P, dw_pre=P, rows=8, n=64, ld=(64,) * 6, per=4,
               dtype=rov.BF16, eps=1e-5, ws=P, ws_bytes=1 << 30):
     return rov.load().rov_norm_residual_bwd(y, h, w_post, gate, w_pre, dy, dn, dx, dh, dw_post, dgate, dw_pre, rows, n, (ctypes.c_int64 * 6)(*ld), per,
                                             dtype, 1.0, 1.0, eps, ws, ws_bytes, None)
@@ -57,6 +58,7 @@ def _norm_bwd(y=P, h=P, w_post=P, gate=P, w_pre=P, dy=P, dn=P, dx=P, dh=P, dw_po
     (dict(dx=0, dh=0, dw_post=0, dgate=0, dw_pre=0), INVALID), (dict(rows=0), INVALID), (dict(per=5), INVALID), (dict(eps=-1.0), INVALID),
     (dict(n=40000, ld=(40000,) * 6), UNSUPPORTED), (dict(ld=(64, 64, 64, 64, 64, 8)), INVALID), (dict(ws=0), INVALID), (dict(ws=P + 4), INVALID),
     (dict(ws_bytes=16), WORKSPACE), (dict(dw_post=P + 2), INVALID), (dict(dtype=rov.FP8_E4M3), UNSUPPORTED),
+    (dict(dh=5 * P), INVALID), (dict(dx=3 * P, ld=(64, 64, 64, 64, 72, 64)), INVALID),
 ])
 def test_norm_residual_bwd_refuses(kw, code):
     assert _norm_bwd(**kw) == code
