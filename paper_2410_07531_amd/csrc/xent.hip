@@ -11,7 +11,7 @@
 // loads.  dX is summed over the pieces, and either over shares of k where its tiles alone would leave compute units idle, in fp32.
 // G is rounded to bf16 without its row's factor dloss: with the factor in it, the entries of the targets, which are the bulk of it and
 // nearly the same number -dloss in every row of a mean, would all be off by the same part of up to 2^-9, and so would dX and dW (0.0033 of
-// their norm, 0.0021 without).  dX is multiplied by its row's factor in fp32; for dW the rows of X are multiplied by theirs over the largest,
+// their norm at 8192 x 131072 x 4096, 0.0017 without).  dX is multiplied by its row's factor in fp32; for dW the rows of X are multiplied by theirs over the largest,
 // which changes nothing where they are all the same, and dW by the largest.
 // fp32: the fp32 products of gemm_ring.hip; a piece's logits live in the workspace while they are reduced, or turned into G in place.
 #include <hip/hip_runtime.h>
@@ -517,9 +517,11 @@ constexpr float kLog2e = 1.44269504088896341f;
 
 // Operands are addressed with 32-bit byte offsets: 256 rows, or all rows of k of the products for dX (a piece of W, packed where its
 // own rows reach too far) and dW (X times its factors, G).
-int check_head(int M, int64_t ldx, int64_t ldw, const HeadLayout& l, bool backward) {
+int check_head(int M, int V, int64_t ldx, int64_t ldw, const HeadLayout& l, bool backward) {
     const int64_t ld = ldx > ldw ? ldx : ldw;
     if (512 * up_to(ld, 8) > kPanel || 512 * l.kp > kPanel) return ROV_ERR_UNSUPPORTED;
+    const int64_t widest = V > l.kp ? V : l.kp, longest = M > V ? M : V;
+    if (up_to(longest, 256) / 256 * (up_to(widest, 128) / 128) > 0x7FFFFFFF) return ROV_ERR_UNSUPPORTED;   // tiles of any of the products
     if (backward && (up_to(l.packed, 64) * 2 * l.kp > kPanel || up_to(M, 64) * 2 * l.kp > kPanel || up_to(M, 64) * 2 * up_to(l.piece, 64) > kPanel))
         return ROV_ERR_UNSUPPORTED;
     return ROV_OK;
@@ -667,7 +669,7 @@ extern "C" int rov_linear_xent(const void* X, const void* W, const int64_t* targ
     if (workspace == nullptr || !aligned(workspace, kAlign)) return ROV_ERR_INVALID;
     if (dtype == ROV_BF16) {
         const HeadLayout hl = head_layout(M, V, K, vocab_piece, false);
-        ROV_STEP(check_head(M, ldx, ldw, hl, false));
+        ROV_STEP(check_head(M, V, ldx, ldw, hl, false));
         if (workspace_bytes < hl.total) return ROV_ERR_WORKSPACE;
         return head_forward(X, W, targets, M, V, K, ldx, ldw, scale, ignore_index, loss, lse, (char*)workspace, hl, (hipStream_t)stream);
     }
@@ -707,7 +709,7 @@ extern "C" int rov_linear_xent_bwd(const void* X, const void* W, const int64_t* 
     if (workspace == nullptr || !aligned(workspace, kAlign)) return ROV_ERR_INVALID;
     if (dtype == ROV_BF16) {
         const HeadLayout hl = head_layout(M, V, K, vocab_piece, true);
-        ROV_STEP(check_head(M, ldx, ldw, hl, true));
+        ROV_STEP(check_head(M, V, ldx, ldw, hl, true));
         if (workspace_bytes < hl.total) return ROV_ERR_WORKSPACE;
         return head_backward(X, W, targets, lse, dloss, dlse, M, V, K, ldx, ldw, scale, ignore_index, dX, dW, lddx, lddw, (char*)workspace, hl,
                              (hipStream_t)stream);
