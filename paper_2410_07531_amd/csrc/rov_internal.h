@@ -107,8 +107,8 @@ int launch_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, void* 
                            float scaleA, float scaleWg, float scaleWu, float scaleC, hipStream_t stream);
 int check_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, const void* C, int M, int N, int K,
                           float scaleC);
-// The products of the loss over the vocabulary (bf16, fp32 accumulation; strides ld_a, ld_w in bytes, multiples of 16), as forms of the
-// 256-row kernel with other epilogues.  A [M,K], W [N,K], K contiguous, K % 8 == 0:
+// The products of the loss over the vocabulary (bf16, fp32 accumulation; strides ld_a, ld_w in bytes, multiples of 16): gemm_head.hip.
+//  A [M,K], W [N,K], K contiguous, K % 8 == 0:
 //   HEAD_STATS  z = A W^T * alpha (logits in units of log 2): per row and half tile (of 256 or 128 columns) maximum and sum of exp2 to
 //               part[gemm_head_parts(M, N)][M], the target's z to picked[m] (rows whose target is one of the N columns, v0 the first);
 //   HEAD_GRAD   G[m][n] = rows[m].y * exp2(z - rows[m].x) - [v0 + n == target] * rows[m].z in bf16 to g [M][ld_g]; rows[m].w: the bits of the

@@ -4,7 +4,7 @@
 // 2 M V K operations forward and 6 backward, which makes the logits again: matrix cores bound both, but for few rows, where
 // W's bytes do.
 //
-// bf16: the 256-row kernel of gemm.hip with its own epilogues.  Forward, a tile's logits are reduced in the accumulators to a
+// bf16: the 256-row tile of gemm_head.hip.  Forward, a tile's logits are reduced in the accumulators to a
 // maximum and a sum of exponentials per row and 128 columns, which a second kernel joins; nothing else leaves the tile.  Backward
 // walks the vocabulary in pieces: the accumulators of a piece's logits become G, stored in bf16 (the tile's columns are dealt to the lanes so
 // that G leaves in 16-byte stores), and the products for dX and dW read G, W and X as they lie, k across the rows, through transposing LDS
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
 }
 
 // dW [V][K] (rows of ldo) = factor[0] * scale * G^T X over at most 64 * SLOTS rows: G [M][ldg], X [M][ldx], both with rows of whole 16-byte chunks.
-// What bounds it: dW's bytes.  A 256 x 256 tile of gemm.hip has one or two slots of 64 rows to walk here, and with one workgroup a compute unit
+// What bounds it: dW's bytes.  A 256 x 256 tile of gemm_head.hip has one or two slots of 64 rows to walk here, and with one workgroup a compute unit
 // nothing runs while its operands travel and its results leave.  Here a workgroup keeps 128 columns of X in registers, walks over
 // tiles of 128 columns of G, the next of which is on its way, and three (two) workgroups share a compute unit.  131072 x 4096, us, 256 x 256
 // tiles / this: 16 rows 425 / 259 (4.1 TB/s), 64 rows 462 / 288, 128 rows 515 / 360.
