@@ -548,7 +548,7 @@ int rov_block_forward_static(const rov_block_weights *w, const void *x, void *y,
  * Element (b, s, h, e) of Q lives at Q[b*strides[0] + s*strides[1] + h*strides[2] + e], of Qo with strides[3..5], of
  * K with strides[6..8], of Ko with strides[9..11]; strides in elements, the head dimension is contiguous.
  * Qo may be Q and Ko may be K (in place, with equal strides, else ROV_ERR_INVALID); otherwise results must not
- * overlap inputs.  Hkv == 0: no keys (K, Ko ignored).  dtype ROV_F32 or ROV_BF16; arithmetic in fp32.
+ * overlap inputs or each other.  Hkv == 0: no keys (K, Ko ignored).  dtype ROV_F32 or ROV_BF16; arithmetic in fp32.
  * positions: device, position of token (b, s) at positions[b*positions_stride + s] (stride 0: one row for all
  * sequences), any value whose angle is below 2^30; NULL: token s is at position s.  Angles are formed in double.
  * cfg lies in host memory.  rot even, 0 < rot <= d; d > 512: ROV_ERR_UNSUPPORTED. */
@@ -641,7 +641,7 @@ int rov_linear_xent(const void *X, const void *W, const int64_t *targets, int M,
 
 /* Its gradients, from the lse of the forward call and the gradients of loss and (may be NULL) lse:
  *     G = scale * (softmax(z) * (dloss + dlse) - onehot(target) * dloss),   dX = G W,   dW = G^T X,
- * in the dtype of X and W, row strides lddx, lddw (>= K).  dX or dW may be NULL.  fp32 accumulation; for bf16, G without its
+ * in the dtype of X and W, row strides lddx, lddw (>= K), in buffers of their own.  dX or dW may be NULL.  fp32 accumulation; for bf16, G without its
  * row's factor and (for dW) the rows of X times it are rounded to bf16 for the matrix products.  Every element of dX and dW is written.  The logits are made a second time. */
 int rov_linear_xent_bwd(const void *X, const void *W, const int64_t *targets, const float *lse,
                         const float *dloss, const float *dlse, int M, int V, int K, int64_t ldx, int64_t ldw,

@@ -533,11 +533,35 @@ def make_block_weights(w, w_scale=None):
 
 def make_block_opts(rope=None, positions=None, post1=None, gate1=None, post2=None, gate2=None, rows_per_gate=0, x_scale=1.0, h_scale=1.0):
     """Rotary form (make_rope_cfg; positions int64 [B, S] or [S]), post norms, gates and residual scales of a block (rov_block_opts).
-    The caller keeps the tensors; the opts keep the rotary form."""
-    ptr = lambda t: t.data_ptr() if t is not None else None
-    stride = positions.stride(0) if positions is not None and positions.dim() == 2 and positions.shape[0] > 1 else 0
-    return BlockOpts(ctypes.pointer(rope) if rope is not None else None, ptr(positions), stride, ptr(post1), ptr(gate1), ptr(post2), ptr(gate2),
+    The opts keep the tensors and the rotary form."""
+    names, tensors = ("post1", "gate1", "post2", "gate2"), (post1, gate1, post2, gate2)
+    stride = 0
+    if any(t is not None for t in tensors + (positions,)):
+        _on_gpu("make_block_opts", None, names + ("positions",), tensors + (positions,))
+        for name, t in zip(names, tensors):
+            if t is not None and (t.dtype != _torch.bfloat16 or not t.is_contiguous()):
+                raise TypeError("make_block_opts: %s must be torch.bfloat16, contiguous" % name)
+    if positions is not None:
+        if positions.dtype != _torch.int64:
+            raise TypeError("make_block_opts: positions must be torch.int64, not %s" % positions.dtype)
+        if positions.dim() not in (1, 2) or (positions.shape[-1] > 1 and positions.stride(-1) != 1):
+            raise ValueError("make_block_opts: positions must be [B, S], [1, S] or [S], contiguous along S")
+        stride = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
+    opts = BlockOpts(ctypes.pointer(rope) if rope is not None else None, _ptr(positions), stride, _ptr(post1), _ptr(gate1), _ptr(post2), _ptr(gate2),
                      int(rows_per_gate), float(x_scale), float(h_scale))
+    opts.tensors = (positions,) + tensors
+    return opts
+
+
+def _check_block_opts(opts, B, S, hidden):
+    """Does what the opts point at have the elements that the block reads?"""
+    positions, post1, gate1, post2, gate2 = getattr(opts, "tensors", (None,) * 5)   # (a BlockOpts of the caller's own has none)
+    if positions is not None and positions.shape not in ((B, S), (1, S), (S,)):
+        raise ValueError("block_forward: positions must be [B, S], [1, S] or [S]")
+    gates = B * S // opts.rows_per_gate if opts.rows_per_gate > 0 else 1
+    for name, have, want in (("post1", post1, hidden), ("gate1", gate1, gates * hidden), ("post2", post2, hidden), ("gate2", gate2, gates * hidden)):
+        if have is not None and have.numel() != want:
+            raise ValueError("block_forward: %s must have %d elements, not %d" % (name, want, have.numel()))
 
 
 def block_forward(weights, x, y, cfg, schedule, seed, offset, mask, workspace, main_stream, side_stream,
@@ -549,6 +573,7 @@ def block_forward(weights, x, y, cfg, schedule, seed, offset, mask, workspace, m
     rest = (x.data_ptr(), y.data_ptr(), B, S, ctypes.byref(cfg), int(schedule), seed & (2**64 - 1), offset & (2**64 - 1), int(mask_ready),
             mptr, nptr, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(main_stream), _stream_ptr(side_stream))
     if opts is not None:
+        _check_block_opts(opts, B, S, cfg.hidden)
         _check(load().rov_block_forward_opts(ctypes.byref(weights), ctypes.byref(opts), *rest), "rov_block_forward_opts")
     else:
         _check(load().rov_block_forward(ctypes.byref(weights), *rest), "rov_block_forward")
@@ -710,7 +735,6 @@ def _rows_per_gate(what, rows, n, w_pre, w_post, gate):
 
 def _ptr(t):
     return t.data_ptr() if t is not None else None
-
 
 
 def norm_residual(x, h, w_pre=None, w_post=None, gate=None, x_scale=1.0, h_scale=1.0, eps=1e-5, y=None, yn=None, yn_fp8_scale=None,

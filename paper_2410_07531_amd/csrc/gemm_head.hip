@@ -424,7 +424,7 @@ int launch_head_part(int kind, int nj, const void* A, const void* W, void* C, in
     const int rc = set_max_dynamic_lds((const void*)kern, kLdsBytes);
     if (rc != ROV_OK) return rc;
     const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + 32 * nj - 1) / (32 * nj);
-    if (tiles_m * tiles_n > 0x7FFFFFFFLL) return ROV_ERR_UNSUPPORTED;
+    if (!grid_fits(tiles_m * tiles_n, 256)) return ROV_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
                        (uint16_t*)C, M, N, K, alpha, (int)tiles_m, (int)tiles_n, head);
     ROV_LAUNCH_CHECK();

@@ -525,6 +525,7 @@ int launch_norm_residual(const void* x, const void* h, const void* w_post, const
     for (const void* q : all) vec = vec && aligned(q, 16);
     for (int i = 0; i < 3; ++i) vec = vec && ld[i] % w == 0;
     if (yn != nullptr) vec = vec && ld[3] % w == 0 && aligned(yn, 8);
+    if (!grid_fits(rows, row_shape(vec ? n / w : n, vec ? w : 1).nt)) return ROV_ERR_UNSUPPORTED;
     if (dtype == ROV_F32) vec ? launch_fwd<float, 4, false>(p, stream) : launch_fwd<float, 1, false>(p, stream);
     else if (out8) vec ? launch_fwd<uint16_t, 8, true>(p, stream) : launch_fwd<uint16_t, 1, true>(p, stream);
     else vec ? launch_fwd<uint16_t, 8, false>(p, stream) : launch_fwd<uint16_t, 1, false>(p, stream);

@@ -171,7 +171,7 @@ int launch_form(RopeParams& p, hipStream_t stream) {
     p.inv_token_units = inverse(tpb * token_units, token_units);
     p.inv_units = inverse(token_units, units);
     const int64_t blocks = (p.tokens + tpb - 1) / tpb;
-    if (blocks > 0x7FFFFFFF) return ROV_ERR_UNSUPPORTED;
+    if (!grid_fits(blocks, 256)) return ROV_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((rope_kernel<T, W, HALVES>), dim3((unsigned)blocks), dim3(256), (size_t)tpb * p.rot * sizeof(float), stream, p);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
@@ -208,6 +208,7 @@ int check_rope(const rov_rope_cfg* c, const void* Q, const void* Qo, const void*
         if ((t ? K : Q) == (t ? Ko : Qo))
             for (int i = 0; i < 3; ++i)
                 if (strides[6 * t + i] != strides[6 * t + 3 + i]) return ROV_ERR_INVALID;
+    if (Hkv > 0 && (Qo == Ko || Qo == K || Ko == Q)) return ROV_ERR_INVALID;   // (turned by two threads, or by one before the other has read it)
     if ((int64_t)H + Hkv > 0x7FFFFFFF / kMaxHead) return ROV_ERR_UNSUPPORTED;
     return rc;
 }

@@ -107,6 +107,8 @@ int launch_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, void* 
                            float scaleA, float scaleWg, float scaleWu, float scaleC, hipStream_t stream);
 int check_gemm_swiglu_fp8(const void* A, const void* Wg, const void* Wu, const void* C, int M, int N, int K,
                           float scaleC);
+// Can a launch have that many workgroups (32-bit numbers of threads)?
+inline bool grid_fits(int64_t groups, int threads) { return groups <= 0x7FFFFFFF && groups * threads <= 0xFFFFFFFFLL; }
 // The products of the loss over the vocabulary (bf16, fp32 accumulation; strides ld_a, ld_w in bytes, multiples of 16): gemm_head.hip.
 //  A [M,K], W [N,K], K contiguous, K % 8 == 0:
 //   HEAD_STATS  z = A W^T * alpha (logits in units of log 2): per row and half tile (of 256 or 128 columns) maximum and sum of exp2 to

@@ -459,7 +459,8 @@ int check_xent(const void* X, const void* W, const int64_t* targets, int M, int 
     if (dtype != ROV_F32 && dtype != ROV_BF16) return dtype == ROV_FP8_E4M3 ? ROV_ERR_UNSUPPORTED : ROV_ERR_INVALID;
     const size_t esz = dtype == ROV_F32 ? 4 : 2;
     if (!aligned(X, esz) || !aligned(W, esz) || !aligned(targets, 8)) return ROV_ERR_INVALID;
-    if (M > (1 << 30) || V > (1 << 30)) return ROV_ERR_UNSUPPORTED;
+    // (fp32: a workgroup a row; bf16: tiles are counted below)
+    if (V > (1 << 30) || M > (1 << 27) || (dtype == ROV_F32 && !grid_fits(M, 256))) return ROV_ERR_UNSUPPORTED;
     return ROV_OK;
 }
 
@@ -521,7 +522,7 @@ int check_head(int M, int V, int64_t ldx, int64_t ldw, const HeadLayout& l, bool
     const int64_t ld = ldx > ldw ? ldx : ldw;
     if (512 * up_to(ld, 8) > kPanel || 512 * l.kp > kPanel) return ROV_ERR_UNSUPPORTED;
     const int64_t widest = V > l.kp ? V : l.kp, longest = M > V ? M : V;
-    if (up_to(longest, 256) / 256 * (up_to(widest, 128) / 128) > 0x7FFFFFFF) return ROV_ERR_UNSUPPORTED;   // tiles of any of the products
+    if (!grid_fits(up_to(longest, 256) / 256 * (up_to(widest, 128) / 128), 256)) return ROV_ERR_UNSUPPORTED;   // tiles of any of the products
     if (backward && (up_to(l.packed, 64) * 2 * l.kp > kPanel || up_to(M, 64) * 2 * l.kp > kPanel || up_to(M, 64) * 2 * up_to(l.piece, 64) > kPanel))
         return ROV_ERR_UNSUPPORTED;
     return ROV_OK;
@@ -665,7 +666,7 @@ extern "C" int rov_linear_xent(const void* X, const void* W, const int64_t* targ
                                size_t workspace_bytes, void* stream) {
     using namespace rov;
     ROV_STEP(check_xent(X, W, targets, M, V, K, ldx, ldw, dtype, scale, ignore_index, vocab_piece));
-    if (loss == nullptr || lse == nullptr || !aligned(loss, 4) || !aligned(lse, 4)) return ROV_ERR_INVALID;
+    if (loss == nullptr || lse == nullptr || loss == lse || !aligned(loss, 4) || !aligned(lse, 4)) return ROV_ERR_INVALID;
     if (workspace == nullptr || !aligned(workspace, kAlign)) return ROV_ERR_INVALID;
     if (dtype == ROV_BF16) {
         const HeadLayout hl = head_layout(M, V, K, vocab_piece, false);
@@ -702,7 +703,7 @@ extern "C" int rov_linear_xent_bwd(const void* X, const void* W, const int64_t* 
                                    size_t workspace_bytes, void* stream) {
     using namespace rov;
     ROV_STEP(check_xent(X, W, targets, M, V, K, ldx, ldw, dtype, scale, ignore_index, vocab_piece));
-    if (lse == nullptr || dloss == nullptr || (dX == nullptr && dW == nullptr)) return ROV_ERR_INVALID;
+    if (lse == nullptr || dloss == nullptr || dX == dW) return ROV_ERR_INVALID;
     if (!aligned(lse, 4) || !aligned(dloss, 4) || !aligned(dlse, 4)) return ROV_ERR_INVALID;
     const size_t esz = dtype == ROV_F32 ? 4 : 2;
     if ((dX != nullptr && (lddx < K || !aligned(dX, esz))) || (dW != nullptr && (lddw < K || !aligned(dW, esz)))) return ROV_ERR_INVALID;

@@ -142,6 +142,38 @@ def test_block_option_errors():
     assert bool((y == 3.0).all())
 
 
+def test_block_options_that_would_be_read_beyond_their_end():
+    B, S = 2, 64
+    x, w, around, pos = _setup(B, S, 75)
+    cfg = rov.make_block_cfg(*(DIMS[k] for k in ("H", "Hkv", "d", "hidden", "ffn")), 0.0)
+    ws = torch.empty(rov.block_workspace_bytes(cfg, B, S, 0), dtype=torch.uint8, device="cuda")
+    y, hidden = torch.full_like(x, 3.0), DIMS["hidden"]
+    gate = torch.ones(1, hidden, dtype=torch.bfloat16, device="cuda")
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    form = rov.make_rope_cfg(128, 1e4)
+    at = torch.zeros(B, 2 * S, dtype=torch.int64, device="cuda")
+    torch.cuda.synchronize()
+    for kw in (dict(rope=form, positions=at[:, :S].int()), dict(post1=gate[0].float()), dict(gate2=torch.ones(1, 2 * hidden, dtype=torch.bfloat16, device="cuda")[:, ::2])):
+        with pytest.raises(TypeError):
+            rov.make_block_opts(**kw)
+    for kw in (dict(rope=form, positions=at[:, ::2]), dict(rope=form, positions=at[0].cpu()), dict(gate1=gate.cpu())):
+        with pytest.raises(ValueError):
+            rov.make_block_opts(**kw)
+    for kw in (dict(rope=form, positions=at[0, :S - 1]), dict(rope=form, positions=at[:1, :S - 1]), dict(post2=gate[0, :-8]), dict(gate1=gate, rows_per_gate=S),
+               dict(gate2=gate.repeat(2, 1))):
+        with pytest.raises(ValueError):
+            rov.block_forward(rov.make_block_weights(w), x, y, cfg, rov.SCHED_FUSED, 1, 0, None, ws, main, side, opts=rov.make_block_opts(**kw))
+    torch.cuda.synchronize()
+    assert bool((y == 3.0).all())
+    # one row of positions for all sequences, a view, and a gate a sequence are taken
+    two = gate.repeat(2, 1)
+    torch.cuda.synchronize()
+    for kw in (dict(rope=form, positions=at[:1, :S]), dict(rope=form, positions=at[:, :S]), dict(gate1=two, rows_per_gate=S)):
+        rov.block_forward(rov.make_block_weights(w), x, y, cfg, rov.SCHED_FUSED, 1, 0, None, ws, main, side, opts=rov.make_block_opts(**kw))
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(y).all())
+
+
 def test_training_tail_forward_and_back():
     # hidden states -> norm around the branch -> loss over the vocabulary, and back; beside it queries turned by their positions and their
     # gradient turned back.  Against automatic differentiation in 64 bits; every tensor between two operators is rounded to bf16 (half a

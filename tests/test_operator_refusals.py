@@ -26,6 +26,8 @@ def _rope(cfg=None, Q=P, Qo=2 * P, K=3 * P, Ko=4 * P, B=1, S=4, H=2, Hkv=1, d=64
     (dict(scaling=rov.ROPE_SCALE_PARTS, factor=8.0, trained_len=8, turns_low=4.0, turns_high=4.0), INVALID),
     (dict(magnitude=float("nan")), INVALID), (dict(dtype=7), INVALID), (dict(dtype=rov.FP8_E4M3), UNSUPPORTED), (dict(d=520, rot=64), UNSUPPORTED),
     (dict(Q=P + 1), INVALID), (dict(positions=P + 4), INVALID), (dict(Qo=P, strides=[512, 128, 64, 512, 128, 32] + [256, 64, 64] * 2), INVALID),   # in place, other strides
+    (dict(Ko=2 * P), INVALID), (dict(Ko=P), INVALID), (dict(Qo=3 * P), INVALID),   # results over each other, over the other's input
+    (dict(S=1 << 30, H=1, Hkv=0, rot=256, d=256, strides=[1 << 39, 512, 256] * 4), UNSUPPORTED),   # more workgroups than a launch has
 ])
 def test_rope_refuses(kw, code):
     assert _rope(**kw) == code
@@ -41,6 +43,7 @@ def _norm(x=P, h=2 * P, w_post=P, gate=P, w_pre=P, y=3 * P, yn=4 * P, rows=8, n=
     (dict(xs=float("inf")), INVALID), (dict(dtype=9), INVALID), (dict(dtype=rov.FP8_E4M3), UNSUPPORTED), (dict(n=40000, ld=(40000,) * 4), UNSUPPORTED),
     (dict(ld=(64, 63, 64, 64)), INVALID), (dict(fp8=-1.0), INVALID), (dict(fp8=1.0, dtype=rov.F32), UNSUPPORTED), (dict(x=P + 1), INVALID),
     (dict(yn=3 * P), INVALID), (dict(fp8=1.0, yn=P), INVALID), (dict(y=P, ld=(64, 64, 72, 64)), INVALID), (dict(yn=2 * P, ld=(64, 72, 64, 64)), INVALID),
+    (dict(rows=1 << 27, n=512, ld=(512,) * 4), UNSUPPORTED),   # more workgroups than a launch has
 ])
 def test_norm_residual_refuses(kw, code):
     assert _norm(**kw) == code
@@ -64,7 +67,7 @@ def test_norm_residual_bwd_refuses(kw, code):
     assert _norm_bwd(**kw) == code
 
 
-def _xent(X=P, W=P, t=P, M=4, V=10, K=8, ldx=8, ldw=8, dtype=rov.BF16, scale=1.0, ignore=-100, loss=P, lse=P, piece=0, ws=P, ws_bytes=1 << 30):
+def _xent(X=P, W=P, t=P, M=4, V=10, K=8, ldx=8, ldw=8, dtype=rov.BF16, scale=1.0, ignore=-100, loss=5 * P, lse=6 * P, piece=0, ws=P, ws_bytes=1 << 30):
     return rov.load().rov_linear_xent(X, W, t, M, V, K, ldx, ldw, dtype, scale, ignore, loss, lse, piece, ws, ws_bytes, None)
 
 
@@ -73,12 +76,13 @@ def _xent(X=P, W=P, t=P, M=4, V=10, K=8, ldx=8, ldw=8, dtype=rov.BF16, scale=1.0
     (dict(V=0), INVALID), (dict(K=-1), INVALID), (dict(ldx=7), INVALID), (dict(ldw=7), INVALID), (dict(ignore=3), INVALID),
     (dict(scale=float("nan")), INVALID), (dict(piece=-1), INVALID), (dict(dtype=5), INVALID), (dict(dtype=rov.FP8_E4M3), UNSUPPORTED),
     (dict(ws=0), INVALID), (dict(ws=P + 16), INVALID), (dict(ws_bytes=64), WORKSPACE), (dict(X=P + 1), INVALID), (dict(t=P + 4), INVALID),
+    (dict(lse=5 * P), INVALID), (dict(M=1 << 24, dtype=rov.F32), UNSUPPORTED), (dict(M=1 << 26, V=1 << 20), UNSUPPORTED),
 ])
 def test_linear_xent_refuses(kw, code):
     assert _xent(**kw) == code
 
 
-def _xent_bwd(X=P, W=P, t=P, lse=P, dloss=P, dlse=P, M=4, V=10, K=8, ldx=8, ldw=8, dtype=rov.BF16, ignore=-100, dX=P, dW=P, lddx=8, lddw=8, piece=0,
+def _xent_bwd(X=P, W=P, t=P, lse=P, dloss=P, dlse=P, M=4, V=10, K=8, ldx=8, ldw=8, dtype=rov.BF16, ignore=-100, dX=5 * P, dW=6 * P, lddx=8, lddw=8, piece=0,
               ws=P, ws_bytes=1 << 30):
     return rov.load().rov_linear_xent_bwd(X, W, t, lse, dloss, dlse, M, V, K, ldx, ldw, dtype, 1.0, ignore, dX, dW, lddx, lddw, piece, ws, ws_bytes, None)
 
@@ -86,7 +90,7 @@ def _xent_bwd(X=P, W=P, t=P, lse=P, dloss=P, dlse=P, M=4, V=10, K=8, ldx=8, ldw=
 @pytest.mark.parametrize("kw,code", [
     (dict(X=0), INVALID), (dict(lse=0), INVALID), (dict(dloss=0), INVALID), (dict(dX=0, dW=0), INVALID), (dict(lddx=7), INVALID), (dict(lddw=4), INVALID),
     (dict(ignore=9), INVALID), (dict(dX=P + 1), INVALID), (dict(ws=0), INVALID), (dict(ws_bytes=64), WORKSPACE), (dict(dtype=rov.FP8_E4M3), UNSUPPORTED),
-    (dict(dlse=P + 2), INVALID), (dict(K=0), INVALID),
+    (dict(dlse=P + 2), INVALID), (dict(K=0), INVALID), (dict(dW=5 * P), INVALID),
 ])
 def test_linear_xent_bwd_refuses(kw, code):
     assert _xent_bwd(**kw) == code
