@@ -383,29 +383,40 @@ __global__ __launch_bounds__(256, 1) void gemm_head_kernel(const char* __restric
             __builtin_amdgcn_sched_barrier(0);
             const int m = m0 + wm * 128 + i * 16 + mrow;
             if (m >= M) continue;
+            if (sums != nullptr) {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int n = n0 + wn * 16 * NJ + j * 16 + nsub;
-                if (n >= N) continue;
-                f32x4 c;
+                for (int j = 0; j < NJ; ++j) {
+                    const int n = n0 + wn * 16 * NJ + j * 16 + nsub;
+                    if (n >= N) continue;
+                    f32x4 c;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) c[e] = acc_read(acc[j][i][e]);
-                if (sums != nullptr) {
+                    for (int e = 0; e < 4; ++e) c[e] = acc_read(acc[j][i][e]);
                     f32x4* const at = reinterpret_cast<f32x4*>(sums + (size_t)m * head.ld_sum + n);   // (rows are padded to four columns)
                     if (head.add) c += *at;
                     *at = c;
-                } else {
-                    uint16_t* const out = C + (size_t)m * head.ld_out + n;
-                    const float f = times[i];
-                    const uint2 v = make_uint2(pack_bf16x2(f * c[0], f * c[1]), pack_bf16x2(f * c[2], f * c[3]));
-                    if (head.out_wide && n + 3 < N) {
-                        *reinterpret_cast<uint2*>(out) = v;
-                    } else {
-                        const uint32_t h[4] = {v.x & 0xFFFFu, v.x >> 16, v.y & 0xFFFFu, v.y >> 16};
+                }
+                continue;
+            }
+            // rows of 16 lanes swap halves of two blocks: a lane has eight neighbours of one of them, four lanes 64 bytes of a row
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (n + e < N) out[e] = (uint16_t)h[e];
-                    }
+            for (int j = 0; j < NJ; j += 2) {
+                uint32_t w[2][2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        w[b][e] = pack_bf16x2(times[i] * acc_read(acc[j + b][i][2 * e]), times[i] * acc_read(acc[j + b][i][2 * e + 1]));
+                const auto lo = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
+                const auto hi = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
+                const uint32_t v[4] = {lo[0], hi[0], lo[1], hi[1]};
+                const int n = n0 + wn * 16 * NJ + (j + ((lane >> 4) & 1)) * 16 + (lane >> 5) * 8;
+                uint16_t* const out = C + (size_t)m * head.ld_out + n;
+                if (n + 7 < N) {
+                    __builtin_memcpy(out, v, 16);   // (one store, whatever the rows' alignment)
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (n + e < N) out[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
                 }
             }
         }

@@ -117,7 +117,7 @@ inline bool grid_fits(int64_t groups, int threads) { return groups <= 0x7FFFFFFF
 //               int target, negative for none, INT_MIN for a row of zeros whatever its logits are; columns N .. g_cols (N rounded up to 64) are zero.
 // W [K,N], N contiguous, and A [M,K] with rows of whole slots (64 values, zero beyond K; HEAD_DX) or [K,M] (HEAD_DW): A W or A^T W;
 // `shares` workgroups a tile take a share of k each and write fp32 (add: add to) sum[share][M][ld_sum]; sum == NULL (one share): bf16
-// to C, rows of ld_out (out_wide: rows on 8 bytes), times factor[factor_step * m] * scale.
+// to C, rows of ld_out, times factor[factor_step * m] * scale.
 enum { HEAD_STATS = 1, HEAD_GRAD = 2, HEAD_DX = 3, HEAD_DW = 4 };
 struct HeadArgs {
     size_t ld_a = 0, ld_w = 0;
@@ -133,7 +133,7 @@ struct HeadArgs {
     float scale = 1.0f;
     float* sum = nullptr;
     int64_t ld_sum = 0, ld_out = 0;
-    bool add = false, out_wide = false;
+    bool add = false;
 };
 int gemm_head_parts(int M, int N);
 int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,

@@ -147,7 +147,7 @@ __global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t* __rest
 // dst [rows][kp] = src, columns K .. kp zero; times factor[r] / factor[rows] where it is given, rows with factor 0 zero whatever they
 // hold.  Eight values a thread.
 __global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restrict__ src, int64_t ld, uint16_t* __restrict__ dst, int64_t rows, int K, int kp,
-                                                        bool wide, const float* __restrict__ factor) {
+                                                        const float* __restrict__ factor) {
     const int chunks = kp / 8;
     const int64_t total = rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restri
         v.zero();
         if (f != 0.0f) {
             const uint16_t* const at = src + r * ld + c;
-            if (wide) {
-                v.load(at);
+            if (c + 7 < K) {
+                __builtin_memcpy(&v.raw, at, 16);   // (one load, whatever the rows' alignment)
             } else {
                 uint32_t h[8];
 #pragma unroll
@@ -229,7 +229,7 @@ typedef __attribute__((address_space(3))) i16x4* lds_i16x4_ptr;
 
 template <int SLOTS>
 __global__ __launch_bounds__(256, SLOTS == 1 ? 3 : 2) void xent_outer_kernel(const uint16_t* __restrict__ G, int64_t ldg, const uint16_t* __restrict__ X, int64_t ldx,
-                                                           uint16_t* __restrict__ out, int64_t ldo, bool out_wide, int V, int K, int M, int tiles_v,
+                                                           uint16_t* __restrict__ out, int64_t ldo, int V, int K, int M, int tiles_v,
                                                            const float* __restrict__ factor, float scale) {
     constexpr int kTile = SLOTS * 64 * 256;
     __shared__ __attribute__((aligned(16))) char lds[2][kTile];
@@ -313,8 +313,8 @@ __global__ __launch_bounds__(256, SLOTS == 1 ? 3 : 2) void xent_outer_kernel(con
                 uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = bf16_pair(times * acc[2 * t + (e >> 1)][i][2 * (e & 1)], times * acc[2 * t + (e >> 1)][i][2 * (e & 1) + 1]);
-                if (out_wide && k + 7 < K) {
-                    *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                if (k + 7 < K) {
+                    __builtin_memcpy(to, w, 16);   // (one store, whatever the rows' alignment)
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
@@ -341,11 +341,15 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const float* __restrict_
         }
         const float f = factor[step * r] * scale;
         const uint32_t lo = bf16_pair(f * s.x, f * s.y), hi = bf16_pair(f * s.z, f * s.w);
-        const uint16_t h[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
+        const uint32_t h[2] = {lo, hi};
         uint16_t* const to = out + r * ldo + c;
+        if (c + 3 < K) {
+            __builtin_memcpy(to, h, 8);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < K) to[e] = h[e];
+            for (int e = 0; e < 4; ++e)
+                if (c + e < K) to[e] = (uint16_t)(h[e >> 1] >> (16 * (e & 1)));
+        }
     }
 }
 
@@ -465,9 +469,7 @@ int check_xent(const void* X, const void* W, const int64_t* targets, int M, int 
 }
 
 int pack(const void* src, int64_t ld, void* dst, int64_t rows, int K, int64_t kp, const float* factor, hipStream_t st) {
-    const bool wide = K % 8 == 0 && ld % 8 == 0 && aligned(src, 16);
-    hipLaunchKernelGGL(xent_pack_kernel, dim3(sweep_grid(rows * kp / 8)), dim3(256), 0, st, (const uint16_t*)src, ld, (uint16_t*)dst, rows, K, (int)kp, wide,
-                       factor);
+    hipLaunchKernelGGL(xent_pack_kernel, dim3(sweep_grid(rows * kp / 8)), dim3(256), 0, st, (const uint16_t*)src, ld, (uint16_t*)dst, rows, K, (int)kp, factor);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
 }
@@ -491,7 +493,6 @@ int product(int kind, const void* A, int64_t lda, const void* W, int64_t ldw, vo
     h.ld_sum = lds;
     h.add = add;
     h.ld_out = ldo;
-    h.out_wide = aligned(out, 8) && ldo % 4 == 0;
     const int rc = launch_gemm_head(kind, A, W, out, M, N, K, 1.0f, shares, h, st);
     if (rc != ROV_OK || sum == nullptr || !last) return rc;
     return fold(sum, shares, lds, out, ldo, M, N, factor, step, scale, st);
@@ -502,13 +503,12 @@ int outer(const void* G, int64_t ldg, const void* X, int64_t ldx, uint16_t* out,
     int64_t rows = 3 * device_cu_count() / tiles_k;   // as many workgroups as run at once
     if (rows > tiles_v) rows = tiles_v;
     if (rows < 1) rows = 1;
-    const bool wide = aligned(out, 16) && ldo % 8 == 0;
     const dim3 grid((unsigned)tiles_k, (unsigned)rows);
     if (M <= 64)
-        hipLaunchKernelGGL(xent_outer_kernel<1>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v,
+        hipLaunchKernelGGL(xent_outer_kernel<1>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, V, K, M, (int)tiles_v,
                            factor, scale);
     else
-        hipLaunchKernelGGL(xent_outer_kernel<2>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, wide, V, K, M, (int)tiles_v,
+        hipLaunchKernelGGL(xent_outer_kernel<2>, grid, dim3(256), 0, st, (const uint16_t*)G, ldg, (const uint16_t*)X, ldx, out, ldo, V, K, M, (int)tiles_v,
                            factor, scale);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
