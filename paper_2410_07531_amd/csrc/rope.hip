@@ -60,7 +60,7 @@ __device__ __forceinline__ void rope_sincos(const RopeParams& p, int64_t pos, in
 // n / d by a multiplication where that is exact (inv = 2^32 / d rounded up, n * d < 2^32), else inv == 0
 __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t inv) { return inv != 0 ? __umulhi(n, inv) : n / d; }
 
-// W: elements a thread moves at once (16 bytes), or 1 where rows, heads or `rot` are off 16 bytes.
+// W: elements a thread moves at once (16 bytes, from any address), or 1 where heads or `rot` are no whole pieces.
 // A unit of a head is W pairs (split layout: W elements of each half), max(1, W / 2) pairs (adjacent), or W elements to copy; a
 // workgroup's units are those of all heads of its tokens.  A thread loads two units before it waits for anything, the first two
 // before the sines are formed.
@@ -223,14 +223,12 @@ int launch_rope_cfg(const rov_rope_cfg* c, const void* Q, void* Qo, const void* 
     RopeParams p{};
     p.src[0] = Q; p.src[1] = K; p.dst[0] = Qo; p.dst[1] = Ko;
     const int64_t esz = dtype == ROV_F32 ? 4 : 2, w = 16 / esz;
-    bool vec = d % w == 0 && c->rot % (c->layout == ROV_ROPE_HALVES ? 2 * w : w) == 0;
+    const bool vec = d % w == 0 && c->rot % (c->layout == ROV_ROPE_HALVES ? 2 * w : w) == 0;
     bool copy = false;
     for (int t = 0; t < 2; ++t) {
         p.sb[t] = strides[6 * t]; p.ss[t] = strides[6 * t + 1]; p.sh[t] = strides[6 * t + 2];
         p.db[t] = strides[6 * t + 3]; p.ds[t] = strides[6 * t + 4]; p.dh[t] = strides[6 * t + 5];
         if (t == 1 && Hkv == 0) break;
-        vec = vec && aligned(p.src[t], 16) && aligned(p.dst[t], 16);
-        for (int i = 0; i < 6; ++i) vec = vec && strides[6 * t + i] % w == 0;
         copy = copy || p.src[t] != p.dst[t];
     }
     p.positions = positions; p.positions_stride = positions_stride;
