@@ -266,3 +266,55 @@ def test_refusals_in_the_binding():
         rov.norm_residual_bwd(x, x, x, None, w_pre=x[0].contiguous())
     with pytest.raises(rov.RovError):
         rov.norm_residual_bwd(x, x, x, x, w_pre=x[0].contiguous(), workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
+# ---- rows of no whole 16-byte pieces, longer than those that move element by element
+RAGGED = [(3, 1025), (5, 1501), (2, 2050), (3, 4099), (2, 8191), (2, 8201), (2, 16381), (1, 32767), (67, 1030)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", RAGGED)
+@pytest.mark.parametrize("gates,post", [(1, True), (-1, True), (0, False)])
+def test_ragged_rows(dtype, rows, n, gates, post):
+    print("norm ragged", dtype, rows, n, gates, post, flush=True)
+    d = make(rows, n, dtype, rows if gates < 0 else gates, post, True)
+    y, yn = rov.norm_residual(d["x"], d["h"], d["w_pre"], d["w_post"], d["gate"], x_scale=0.75, h_scale=0.5, eps=EPS)
+    wy, my, wn, mn = forward(d, 0.75, 0.5)
+    check(y, wy, my, dtype, 2.0 ** -18)
+    check(yn, wn, mn, dtype, 2.0 ** -18)
+    d = make(rows, n, dtype, rows if gates < 0 else gates, post, True, backward=True)
+    got = rov.norm_residual_bwd(d["y"], d["h"], d["dy"], d["dn"], d["w_pre"], d["w_post"], d["gate"], x_scale=0.75, h_scale=0.5, eps=EPS)
+    check_gradients(d, got, 0.75, 0.5, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [512, 1027, 4096, 4101, 9000])
+def test_any_stride_and_address(dtype, n):
+    # in place inside wider rows that start off 16 bytes: the bits of dense rows, and what lies around them stays
+    rows = 4
+    d = make(rows, n, dtype, 2, True, True, seed=9)
+    b = make(rows, n, dtype, 2, True, True, seed=9, backward=True)
+
+    def inside(t):
+        wide = torch.full((rows, n + 7), 3.0, dtype=DT[dtype], device="cuda")
+        wide[:, 3:3 + n] = t
+        return wide, wide[:, 3:3 + n]
+
+    want = rov.norm_residual(d["x"], d["h"], d["w_pre"], d["w_post"], d["gate"])
+    (wx, x), (wh, h) = inside(d["x"]), inside(d["h"])
+    got = rov.norm_residual(x, h, d["w_pre"], d["w_post"], d["gate"], y=x, yn=h)
+    want_b = rov.norm_residual_bwd(b["y"], b["h"], b["dy"], b["dn"], b["w_pre"], b["w_post"], b["gate"])
+    (wd, dy), (we, e) = inside(b["dy"]), inside(b["h"])
+    got_b = rov.norm_residual_bwd(inside(b["y"])[1], e, dy, inside(b["dn"])[1], b["w_pre"], b["w_post"], b["gate"], dx=dy, dh=e)
+    assert all(torch.equal(a, c) for a, c in zip(want, got)) and all(torch.equal(a, c) for a, c in zip(want_b, got_b))
+    for wide in (wx, wh, wd, we):
+        assert bool((wide[:, :3] == 3.0).all()) and bool((wide[:, 3 + n:] == 3.0).all())
+
+
+def test_ragged_rows_into_e4m3_behind_a_guard():
+    d = make(5, 1501, "bf16", 0, True, True)
+    out = torch.full((5, 1505), 7, dtype=torch.uint8, device="cuda")
+    rov.norm_residual(d["x"], d["h"], d["w_pre"], d["w_post"], yn=out[:, :1501], yn_fp8_scale=0.02)
+    want, mag = forward(d, 1.0, 1.0)[2:]
+    err = (out[:, :1501].contiguous().view(torch.float8_e4m3fn).double().cpu() * 0.02 - want).abs()
+    assert bool((err <= 2.0 ** -4 * want.abs() + 2.0 ** -10 * 0.02 + 2.0 ** -17 * mag).all()) and bool((out[:, 1501:] == 7).all())

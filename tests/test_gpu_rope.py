@@ -180,3 +180,18 @@ def test_refusals_in_the_binding():
         rov.rope(cfg, Q, Qo=torch.zeros(1, 2, 2, 32, device="cuda"))
     with pytest.raises(rov.RovError):
         rov.rope(rov.make_rope_cfg(66, 10000.0), Q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [rov.ROPE_INTERLEAVED, rov.ROPE_HALVES])
+def test_any_stride_and_address(dtype, layout):
+    # heads that start off 16 bytes, in place: the bits of dense heads, and what lies around them stays
+    B, S, H, d = 2, 19, 3, 64
+    Q = torch.randn(B, S, H, d, generator=torch.Generator().manual_seed(4)).to(DT[dtype]).cuda()
+    cfg = rov.make_rope_cfg(32, 10000.0, layout=layout)
+    want = rov.rope(cfg, Q)
+    wide = torch.full((B, S, H, d + 5), 3.0, dtype=DT[dtype], device="cuda")
+    at = wide[..., 1:1 + d]
+    at.copy_(Q)
+    rov.rope(cfg, at, Qo=at)
+    assert torch.equal(at, want) and bool((wide[..., :1] == 3.0).all()) and bool((wide[..., 1 + d:] == 3.0).all())
