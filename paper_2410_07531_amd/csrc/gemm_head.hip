@@ -2,15 +2,16 @@
 // two products of their gradients.  bf16 operands, fp32 accumulation, rows of any stride.
 //
 // The main loop is that of the bf16 256-row kernel of gemm.hip (256 x 256 or 256 x 128 tile, four waves in a 2 x 2 grid, MFMA 16x16x32, two
-// 64 KiB LDS slots of 128-byte rows filled by loads that write LDS, fragments read a k-step ahead; its comments say why), with two
+// 64 KiB LDS slots of 128-byte rows filled by loads that write LDS, fragments read a k-step ahead; its comments say why), with three
 // differences:
 //   - the epilogue: HEAD_STATS keeps the row statistics of the tile's logits, HEAD_GRAD turns them into gradients, HEAD_DX and HEAD_DW
 //     store the product, or fp32 sums of it over shares of k;
 //   - HEAD_DX: the second operand lies as [K, N] (rows of k), HEAD_DW: both do.  Such an operand's part of a slot is 64 rows of k by the
 //     tile's columns; fragments come by the transposing LDS load, two a fragment, with the k order of the other operand's.
-// One tile a workgroup.  (As many workgroups as compute units, each of which sends the next tile's first loads out before the epilogue,
-// keep more values alive across the tiles than there are scalar registers: 522 -> 528 us for the loss of 2048 x 32000 x 1024 with gradients,
-// 1540 -> 1550 us for the loss alone of 2048 x 128256 x 4096.)
+//   - a workgroup takes one tile after the other, and the loads of a tile's last two slots' time are the next tile's first: its loop goes on
+//     behind the epilogue as if there were one longer k.  Against a tile a workgroup, us: loss with gradients 1000 x 50257 x 1024 502 / 487, 8192 x
+//     50257 x 1024 3160 / 3046, 4096 x 50304 x 256 770 / 730, 8192 x 131072 x 4096 26050 / 25910; loss alone 2048 x 131072 x 4096 1600 / 1574.  What
+//     the epilogue reads is asked for before the loop, and no wait stands before its stores: loads sent out between loop and epilogue gained nothing.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -106,73 +107,76 @@ __global__ __launch_bounds__(256, 1) void gemm_head_kernel(const char* __restric
     const bool beyond_k = RAGGED && ((lane & 7) ^ swz(wave * 8 + (lane >> 3))) * 16 >= (int)(row_bytes - (size_t)(ns - 1) * kRow);
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lptr_t)lds;
 
-    // XCD-aware tile id: workgroup ids are dealt round-robin to the 8 XCDs; give each XCD a contiguous
-    // range of logical tiles, ordered in bands of 8 tile-rows with the row fastest
-    const int T = gridDim.x, pid = blockIdx.x, per = T >> 3, rem = T & 7, xcd = pid & 7, loc = pid >> 3;
-    const int id = xcd < rem ? xcd * (per + 1) + loc : rem * (per + 1) + (xcd - rem) * per + loc;
-    constexpr int GM = 8;
-    const int band = id / (GM * tiles_n);
-    const int band_rows = (tiles_m - band * GM) < GM ? (tiles_m - band * GM) : GM;
-    const int in_band = id - band * GM * tiles_n;
-    const int tm = band * GM + in_band % band_rows;
-    const int tn = in_band / band_rows;
-    const int m0 = tm * BM;
-    const int n0 = tn * BNT;
-    const int kstart = (int)((unsigned)tm % (unsigned)ns);   // the slot at which the cyclic walk over k starts: tile-rows that run together read W apart
-    const int rows_a = M - m0 < BM ? M - m0 : BM;
-    const int rows_w = N - n0 < BNT ? N - n0 : BNT;
-    uint32_t voff_a[8], voff_w[NJ];   // lanes' byte offsets of load j of each operand
+    // The tile that the loads are aimed at: lanes' byte offsets of load j of each operand, buffer resources, start of the walk over k
+    uint32_t voff_a[8], voff_w[NJ];
+    i32x4 rsrc_a, rsrc_w;
+    int kstart = 0, aim_m0 = 0, aim_n0 = 0, aim_tn = 0;
+    const int T = tiles_m * tiles_n;
+    auto aim = [&](int pid) __attribute__((always_inline)) {
+        // XCD-aware tile id: workgroup ids are dealt round-robin to the 8 XCDs; give each XCD a contiguous
+        // range of logical tiles, ordered in bands of 8 tile-rows with the row fastest
+        const int per = T >> 3, rem = T & 7, xcd = pid & 7, loc = pid >> 3;
+        const int id = xcd < rem ? xcd * (per + 1) + loc : rem * (per + 1) + (xcd - rem) * per + loc;
+        constexpr int GM = 8;
+        const int band = id / (GM * tiles_n);
+        const int band_rows = (tiles_m - band * GM) < GM ? (tiles_m - band * GM) : GM;
+        const int in_band = id - band * GM * tiles_n;
+        const int tm = band * GM + in_band % band_rows;
+        aim_tn = __builtin_amdgcn_readfirstlane(in_band / band_rows);
+        aim_m0 = __builtin_amdgcn_readfirstlane(tm * BM);
+        aim_n0 = aim_tn * BNT;
+        kstart = __builtin_amdgcn_readfirstlane((int)((unsigned)tm % (unsigned)ns));   // the slot at which the cyclic walk over k starts: tile-rows that run together read W apart
+        const int rows_a = M - aim_m0 < BM ? M - aim_m0 : BM;
+        const int rows_w = N - aim_n0 < BNT ? N - aim_n0 : BNT;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int row = (wave + 4 * j) * 8 + (lane >> 3);
-        const int chunk = (lane & 7) ^ swz(row);
-        // HEAD_GRAD: LDS row 128*h + 16*i + r holds activation row 128*h + 8*r + i, and weight row 32*j + 16*k + 4*g + e (k = 0, 1) weight
-        // row 32*j + 8*g + 4*k + e, so that a lane ends up with eight consecutive rows and groups of eight consecutive columns of the
-        // tile, and the four lanes of a row with 32
-        const int arow = HEAD == HEAD_GRAD ? (row & 128) | ((row & 15) << 3) | ((row >> 4) & 7) : row;
-        const int wrow = HEAD == HEAD_GRAD ? (row & ~31) | (((row >> 2) & 3) << 3) | (((row >> 4) & 1) << 2) | (row & 3) : row;
-        if constexpr (KNA) {   // a load is two rows of k of 256 columns, or four of 128
-            const int krow = (wave + 4 * j) * 2 + (lane >> 5);
-            voff_a[j] = (uint32_t)krow * (uint32_t)ld_a + (uint32_t)(((lane & 31) ^ swz_kn(krow)) * 16);
-        } else {
-            const int ra = arow < rows_a ? arow : rows_a - 1;   // rows past the edge are never stored
-            voff_a[j] = (uint32_t)((size_t)ra * ld_a) + (uint32_t)(chunk * 16);
+        for (int j = 0; j < 8; ++j) {
+            const int row = (wave + 4 * j) * 8 + (lane >> 3);
+            const int chunk = (lane & 7) ^ swz(row);
+            // HEAD_GRAD: LDS row 128*h + 16*i + r holds activation row 128*h + 8*r + i, and weight row 32*j + 16*k + 4*g + e (k = 0, 1) weight
+            // row 32*j + 8*g + 4*k + e, so that a lane ends up with eight consecutive rows and groups of eight consecutive columns of the
+            // tile, and the four lanes of a row with 32
+            const int arow = HEAD == HEAD_GRAD ? (row & 128) | ((row & 15) << 3) | ((row >> 4) & 7) : row;
+            const int wrow = HEAD == HEAD_GRAD ? (row & ~31) | (((row >> 2) & 3) << 3) | (((row >> 4) & 1) << 2) | (row & 3) : row;
+            if constexpr (KNA) {   // a load is two rows of k of 256 columns, or four of 128
+                const int krow = (wave + 4 * j) * 2 + (lane >> 5);
+                voff_a[j] = (uint32_t)krow * (uint32_t)ld_a + (uint32_t)(((lane & 31) ^ swz_kn(krow)) * 16);
+            } else {
+                const int ra = arow < rows_a ? arow : rows_a - 1;   // rows past the edge are never stored
+                voff_a[j] = (uint32_t)((size_t)ra * ld_a) + (uint32_t)(chunk * 16);
+            }
+            if (j >= NJ) continue;
+            if constexpr (KNW) {
+                constexpr int CH = 4 * NJ;   // chunks of a row
+                const int krow = (wave + 4 * j) * (64 / CH) + lane / CH;
+                voff_w[j] = (uint32_t)krow * (uint32_t)ld_w + (uint32_t)(((lane % CH) ^ swz_kn(krow)) * 16);
+            } else {
+                const int rw = wrow < rows_w ? wrow : rows_w - 1;
+                voff_w[j] = (uint32_t)((size_t)rw * ld_w) + (uint32_t)(chunk * 16);
+            }
         }
-        if (j >= NJ) continue;
-        if constexpr (KNW) {
-            constexpr int CH = 4 * NJ;   // chunks of a row
-            const int krow = (wave + 4 * j) * (64 / CH) + lane / CH;
-            voff_w[j] = (uint32_t)krow * (uint32_t)ld_w + (uint32_t)(((lane % CH) ^ swz_kn(krow)) * 16);
-        } else {
-            const int rw = wrow < rows_w ? wrow : rows_w - 1;
-            voff_w[j] = (uint32_t)((size_t)rw * ld_w) + (uint32_t)(chunk * 16);
-        }
-    }
-    // buffer resources over the two panels: scalar base, per-lane 32-bit offset, scalar k offset; the range ends with the last valid row, so
-    // that an offset beyond it reads zeros
-    auto make_rsrc = [](const char* base, size_t bytes) {
-        const uint64_t b = (uint64_t)(uintptr_t)base;
-        i32x4 r;
-        r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)b);
-        r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)((b >> 32) & 0xFFFFu));
-        r[2] = __builtin_amdgcn_readfirstlane((int)(uint32_t)bytes);
-        r[3] = 0x00020000;
-        return r;
+        // buffer resources over the two panels: scalar base, per-lane 32-bit offset, scalar k offset; the range ends with the last valid row, so
+        // that an offset beyond it reads zeros
+        auto make_rsrc = [](const char* base, size_t bytes) {
+            const uint64_t b = (uint64_t)(uintptr_t)base;
+            i32x4 r;
+            r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+            r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)((b >> 32) & 0xFFFFu));
+            r[2] = __builtin_amdgcn_readfirstlane((int)(uint32_t)bytes);
+            r[3] = 0x00020000;
+            return r;
+        };
+        // ([K, N]: up to the last column of the last row of k, in whole chunks, so that rows beyond k read as zeros)
+        auto kn_bytes = [&](size_t ld, int cols) { return (size_t)(k_rows - 1) * ld + (size_t)((cols + 7) / 8 * 16); };
+        rsrc_a = make_rsrc(A + (KNA ? (size_t)aim_m0 * ESZ : (size_t)aim_m0 * ld_a),
+                           KNA ? kn_bytes(ld_a, M - aim_m0) : (size_t)(rows_a - 1) * ld_a + k_bytes);
+        rsrc_w = make_rsrc(Wt + (KNW ? (size_t)aim_n0 * ESZ : (size_t)aim_n0 * ld_w),
+                           KNW ? kn_bytes(ld_w, N - aim_n0) : (size_t)(rows_w - 1) * ld_w + k_bytes);
     };
-    // ([K, N]: up to the last column of the last row of k, in whole chunks, so that rows beyond k read as zeros)
-    auto kn_bytes = [&](size_t ld, int cols) { return (size_t)(k_rows - 1) * ld + (size_t)((cols + 7) / 8 * 16); };
-    const i32x4 rsrc_a = make_rsrc(A + (KNA ? (size_t)m0 * ESZ : (size_t)m0 * ld_a),
-                       KNA ? kn_bytes(ld_a, M - m0) : (size_t)(rows_a - 1) * ld_a + k_bytes);
-    const i32x4 rsrc_w = make_rsrc(Wt + (KNW ? (size_t)n0 * ESZ : (size_t)n0 * ld_w),
-                       KNW ? kn_bytes(ld_w, N - n0) : (size_t)(rows_w - 1) * ld_w + k_bytes);
 
-    // Load instruction q (0..7 = A, 8..7+NJ = W) of slot-step `step` into the slot at LDS byte address `slot`.  Inline assembly, so that
+    // Load instruction q (0..7 = A, 8..7+NJ = W) of the slot at place `st` of k into the slot at LDS byte address `slot`.  Inline assembly, so that
     // the compiler's wait-count pass does not see an LDS write it cannot tell apart from the fragment reads; the waits are placed by hand below.
     // M0 (the LDS base of the transfer) is a reserved register that compiled code only sets right before its own uses.
-    auto issue = [&](int q, int step, uint32_t slot) __attribute__((always_inline)) {
-        int st = step < ns ? step : ns - 1;       // past the end: harmless reload of the last slot
-        st += kstart;
-        st = st >= ns ? st - ns : st;
+    auto issue = [&](int q, int st, uint32_t slot) __attribute__((always_inline)) {
         const int koff = (q < 8 ? KNA : KNW) ? (int)((uint32_t)st * 64u * (uint32_t)(q < 8 ? ld_a : ld_w)) : st * kRow;
         const uint32_t dst = slot + (uint32_t)(q < 8 ? (wave + 4 * q) * 1024 : BM * kRow + (wave + 4 * (q - 8)) * 1024);
         const i32x4 rsrc = q < 8 ? rsrc_a : rsrc_w;
@@ -210,216 +214,247 @@ __global__ __launch_bounds__(256, 1) void gemm_head_kernel(const char* __restric
     constexpr int P0 = NM >= 4 ? (NM - 4) / G + 1 : 0; // load slots idx % G == 3 of a k-step
     constexpr int VMB = HB >= 2 ? (HB - 2) / G + 1 : 0;
     static_assert(HB >= 0 && P1 <= NL && NL - P1 <= P0 && VMB < 16, "load schedule fits the k-steps");
+    auto next_of = [&](int st) { return st + 1 >= ns ? 0 : st + 1; };   // (one slot: it again)
+    aim(blockIdx.x);
+    int st1 = next_of(kstart);   // where in k the next slot-step lies
 #pragma unroll
-    for (int q = 0; q < NL; ++q) issue(q, 0, lds_base);
+    for (int q = 0; q < NL; ++q) issue(q, kstart, lds_base);
 #pragma unroll
-    for (int q = 0; q < P1; ++q) issue(q, 1, lds_base + kSlot);   // its other loads go out in (0,0) like everywhere below
-
-    f32x4 acc[NJ][8];   // [weight-row block j (16 rows)][activation-row block i (16 rows)]
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[j][i][e] = 0.0f;
-    // written as inline assembly with explicit register classes (accumulators in AGPRs, fragments in VGPRs): see gemm.hip
-    auto mfma_one = [&](int h, int j, int i) {
-        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[j][i]) : "v"(wf[h][j]), "v"(af[h][i]));
-    };
-    // vmcnt(P1): slot-step 0 has landed
-    __builtin_amdgcn_s_waitcnt(0x0F70 | P1);
+    for (int q = 0; q < P1; ++q) issue(q, next_of(kstart), lds_base + kSlot);   // its other loads go out in (0,0) like everywhere below
+    __builtin_amdgcn_s_waitcnt(0x0F70 | P1);   // vmcnt(P1): slot-step 0 has landed
     __syncthreads();
 #pragma unroll
     for (int f = 0; f < NF; ++f) read_frag(0, lds, f);
 
-    for (int S = 0; S < ns; ++S) {
-        const char* cur = lds + (S & 1) * kSlot;
-        const char* nxt = lds + ((S + 1) & 1) * kSlot;
-        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): fragments of (S,0)
-#pragma unroll
-        for (int idx = 0; idx < NM; ++idx) {
-            mfma_one(0, idx >> 3, idx & 7);
-            if (idx < 2 * NF && (idx & 1) == 0) read_frag(1, cur, idx >> 1);
-            if (idx % G == 3 && P1 + idx / G < NL) issue(P1 + idx / G, S + 1, lds_base + ((S + 1) & 1) * kSlot);   // the other loads of slot-step S+1
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): fragments of (S,1)
-        __syncthreads();
-#pragma unroll
-        for (int idx = 0; idx < NM; ++idx) {
-            if (idx == HB) {
-                __builtin_amdgcn_s_waitcnt(0x0F70 | VMB);   // vmcnt(VMB)
-                __syncthreads();
-            }
-            mfma_one(1, idx >> 3, idx & 7);
-            if (idx % G == 1) issue(idx / G, S + 2, lds_base + (S & 1) * kSlot);          // loads 0..P1-1 of slot-step S+2
-            if (idx >= HB && ((idx - HB) & 1) == 0) read_frag(0, nxt, (idx - HB) >> 1);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): no LDS load or read may outlive the loop
-    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMA results are in the accumulators before they are read
-
-    // D'[r][c] = C[m = c][n = r]: lane holds activation row lane%16 and weight rows 4*(lane/16) + e
     const int mrow = lane & 15;
     const int nsub = (lane >> 4) * 4;
-    if constexpr (HEAD == HEAD_STATS) {
-        // per row: maximum and sum of exp2 over this wave's 16*NJ columns (logits in units of log 2: alpha carries log2 e), and the
-        // target's logit where it is one of them
-        const int nw = n0 + wn * 16 * NJ;
-        const bool edge = nw + 16 * NJ > N;
-        int limit = N - nw - nsub;   // the lane's columns 16*j + e (counted from nw + nsub) below this exist
-        int tcol[8];   // the targets' columns among the lane's (read here, all at once: between the rows each would wait for its own read)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int m = m0 + wm * 128 + i * 16 + mrow;
-            const int64_t t = m < M ? head.targets[m] - head.v0 - nw : -1;
-            tcol[i] = t >= 0 && t < 16 * NJ && t < N - nw && (((int)t >> 2) & 3) == (lane >> 4) ? (int)t - nsub : -1;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
-            const int m = m0 + wm * 128 + i * 16 + mrow;
-            float v[NJ][4], top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[j][e] = acc_read(acc[j][i][e]);
-            if (edge) {
-                asm volatile("" : "+v"(limit));   // (compared anew for every row: 32 masks kept between rows do not fit the scalar registers)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (16 * j + e >= limit) v[j][e] = -INFINITY;
-            }
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, v[j][e]);
-            top = fmaxf(exchanged<16>(top)[0], exchanged<16>(top)[1]);
-            top = fmaxf(exchanged<32>(top)[0], exchanged<32>(top)[1]);
-            top *= alpha;
-            const float base = top > -INFINITY ? top : 0.0f;   // (no column, or all minus infinity: the sum is 0, not NaN)
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][e], alpha, -base));
-            sum = exchanged<16>(sum)[0] + exchanged<16>(sum)[1];
-            sum = exchanged<32>(sum)[0] + exchanged<32>(sum)[1];
-            if (lane < 16 && m < M) head.part[(size_t)(2 * tn + wn) * M + m] = make_float2(top, sum);
-            if (__ballot(tcol[i] >= 0) != 0) {   // (few rows of few tiles)
-                float z = 0.0f;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) z = tcol[i] == 16 * j + e ? v[j][e] : z;
-                if (tcol[i] >= 0) head.picked[m] = z * alpha;
-            }
-        }
-    }
-    if constexpr (HEAD == HEAD_GRAD) {
-        // gradients of the logits over the row's factor, G[m][n]; rows that are ignored and columns beyond N are zero, so that G can be
-        // walked in whole slots as the next product's k
-        const int mw = m0 + wm * 128 + 8 * mrow;          // first of this lane's eight rows
-        const int nl = n0 + wn * 16 * NJ + 2 * nsub;      // first of its columns nl + 32*j + 0..7
+    int at = 0;   // slot of the slot-step
+    // (what has to be there before is waited for by hand; a fence would wait for an epilogue's stores too)
+    auto barrier = []() __attribute__((always_inline)) { asm volatile("s_barrier" ::: "memory"); };
+    for (int pid = blockIdx.x;; pid += gridDim.x) {
+        const int m0 = aim_m0, n0 = aim_n0, tn = aim_tn;
+        const bool more = pid + (int)gridDim.x < T;   // is there a next tile?
+        // what the epilogue reads, on its way meanwhile
+        int64_t target[8];
         float4 row[8];   // HeadArgs::rows
-#pragma unroll
-        for (int i = 0; i < 8; ++i) row[i] = head.rows[mw + i < M ? mw + i : M - 1];
-        int tcol[8];
-        bool keep[8], whole = n0 + (wn + 1) * 16 * NJ <= N, hit = false;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = __float_as_int(row[i].w);
-            keep[i] = t != INT_MIN;
-            whole = whole && keep[i];
-            const int64_t c = (int64_t)t - head.v0 - nl;   // 32*j + 0..7: this lane's
-            tcol[i] = t >= 0 && c >= 0 && c < 16 * NJ && (c & 31) < 8 ? (int)c : -1;
-            hit = hit || tcol[i] >= 0;
-        }
-        // most waves see neither an ignored row, nor an edge, nor a target
-        const bool plain = __ballot(!whole || hit) == 0;
-#pragma unroll
-        for (int jj = 0; jj < NJ; jj += 2) {
-            __builtin_amdgcn_sched_barrier(0);
-            const int n = nl + 16 * jj;
-            float g[8][8];   // [row][column n + c]
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    g[i][c] = row[i].y * __builtin_amdgcn_exp2f(__builtin_fmaf(acc_read(acc[jj + (c >> 2)][i][c & 3]), alpha, -row[i].x));
-            if (!plain) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        if (tcol[i] == 16 * jj + c) g[i][c] -= row[i].z;
-                        if (!keep[i] || n + c >= N) g[i][c] = 0.0f;
-                    }
-            }
-            if (n < head.g_cols)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (mw + i < M)
-                        *reinterpret_cast<uint4*>(head.g + (size_t)(mw + i) * head.ld_g + n) =
-                            make_uint4(pack_bf16x2(g[i][0], g[i][1]), pack_bf16x2(g[i][2], g[i][3]), pack_bf16x2(g[i][4], g[i][5]),
-                                       pack_bf16x2(g[i][6], g[i][7]));
-        }
-    }
-    if constexpr (KNW) {
-        // fp32 sums of the shares of k, rows of ld_sum values; or the result itself, bf16
-        float* const sums = head.sum != nullptr ? head.sum + (size_t)blockIdx.y * M * head.ld_sum : nullptr;
-        float times[8];   // (read here, once: between the stores each would wait for its own read)
-        if (sums == nullptr)
+        float times[8];
+        if constexpr (HEAD == HEAD_STATS)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int m = m0 + wm * 128 + i * 16 + mrow;
-                times[i] = head.factor[head.factor_step * (m < M ? m : M - 1)] * head.scale;
+                target[i] = m < M ? head.targets[m] : -1;
             }
+        if constexpr (HEAD == HEAD_GRAD)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
-            const int m = m0 + wm * 128 + i * 16 + mrow;
-            if (m >= M) continue;
-            if (sums != nullptr) {
+            for (int i = 0; i < 8; ++i) {
+                const int m = m0 + wm * 128 + 8 * mrow + i;
+                row[i] = head.rows[m < M ? m : M - 1];
+            }
+        if constexpr (KNW)
+            if (head.sum == nullptr)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const int n = n0 + wn * 16 * NJ + j * 16 + nsub;
-                    if (n >= N) continue;
-                    f32x4 c;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) c[e] = acc_read(acc[j][i][e]);
-                    f32x4* const at = reinterpret_cast<f32x4*>(sums + (size_t)m * head.ld_sum + n);   // (rows are padded to four columns)
-                    if (head.add) c += *at;
-                    *at = c;
+                for (int i = 0; i < 8; ++i) {
+                    const int m = m0 + wm * 128 + i * 16 + mrow;
+                    times[i] = head.factor[head.factor_step * (m < M ? m : M - 1)];
                 }
-                continue;
+        f32x4 acc[NJ][8];   // [weight-row block j (16 rows)][activation-row block i (16 rows)]
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][i][e] = 0.0f;
+        // written as inline assembly with explicit register classes (accumulators in AGPRs, fragments in VGPRs): see gemm.hip
+        auto mfma_one = [&](int h, int j, int i) {
+            asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[j][i]) : "v"(wf[h][j]), "v"(af[h][i]));
+        };
+
+        for (int S = 0; S < ns; ++S) {
+            const char* cur = lds + at * kSlot;
+            const char* nxt = lds + (at ^ 1) * kSlot;
+            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): fragments of (S,0)
+            asm volatile("s_nop 3");              // accumulators written just before
+#pragma unroll
+            for (int idx = 0; idx < NM; ++idx) {
+                mfma_one(0, idx >> 3, idx & 7);
+                if (idx < 2 * NF && (idx & 1) == 0) read_frag(1, cur, idx >> 1);
+                if (idx % G == 3 && P1 + idx / G < NL) issue(P1 + idx / G, st1, lds_base + (at ^ 1) * kSlot);   // the other loads of slot-step S+1
+                __builtin_amdgcn_sched_barrier(0);
             }
-            // rows of 16 lanes swap halves of two blocks: a lane has eight neighbours of one of them, four lanes 64 bytes of a row
+            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): fragments of (S,1)
+            barrier();
+            // the slot-step after the next: the next tile's first where this tile's end, past the last tile's end any (harmless)
+            int st2 = next_of(st1);
+            if (more && S == ns - 2) {
+                aim(pid + gridDim.x);
+                st2 = kstart;
+            }
 #pragma unroll
-            for (int j = 0; j < NJ; j += 2) {
-                uint32_t w[2][2];
+            for (int idx = 0; idx < NM; ++idx) {
+                if (idx == HB) {
+                    __builtin_amdgcn_s_waitcnt(0x0F70 | VMB);   // vmcnt(VMB)
+                    barrier();
+                }
+                mfma_one(1, idx >> 3, idx & 7);
+                if (idx % G == 1) issue(idx / G, st2, lds_base + at * kSlot);          // loads 0..P1-1 of slot-step S+2
+                if (idx >= HB && ((idx - HB) & 1) == 0) read_frag(0, nxt, (idx - HB) >> 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            st1 = st2;
+            at ^= 1;
+        }
+        if (!more) __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): no LDS load or read may outlive the workgroup
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMA results are in the accumulators before they are read
+
+        // D'[r][c] = C[m = c][n = r]: lane holds activation row lane%16 and weight rows 4*(lane/16) + e
+        if constexpr (HEAD == HEAD_STATS) {
+            // per row: maximum and sum of exp2 over this wave's 16*NJ columns (logits in units of log 2: alpha carries log2 e), and the
+            // target's logit where it is one of them
+            const int nw = n0 + wn * 16 * NJ;
+            const bool edge = nw + 16 * NJ > N;
+            int limit = N - nw - nsub;   // the lane's columns 16*j + e (counted from nw + nsub) below this exist
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int m = m0 + wm * 128 + i * 16 + mrow;
+                float v[NJ][4], top = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        w[b][e] = pack_bf16x2(times[i] * acc_read(acc[j + b][i][2 * e]), times[i] * acc_read(acc[j + b][i][2 * e + 1]));
-                const auto lo = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
-                const auto hi = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
-                const uint32_t v[4] = {lo[0], hi[0], lo[1], hi[1]};
-                const int n = n0 + wn * 16 * NJ + (j + ((lane >> 4) & 1)) * 16 + (lane >> 5) * 8;
-                uint16_t* const out = C + (size_t)m * head.ld_out + n;
-                if (n + 7 < N) {
-                    __builtin_memcpy(out, v, 16);   // (one store, whatever the rows' alignment)
-                } else {
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (n + e < N) out[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                    for (int e = 0; e < 4; ++e) v[j][e] = acc_read(acc[j][i][e]);
+                if (edge) {
+                    asm volatile("" : "+v"(limit));   // (compared anew for every row: 32 masks kept between rows do not fit the scalar registers)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (16 * j + e >= limit) v[j][e] = -INFINITY;
+                }
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, v[j][e]);
+                top = fmaxf(exchanged<16>(top)[0], exchanged<16>(top)[1]);
+                top = fmaxf(exchanged<32>(top)[0], exchanged<32>(top)[1]);
+                top *= alpha;
+                const float base = top > -INFINITY ? top : 0.0f;   // (no column, or all minus infinity: the sum is 0, not NaN)
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][e], alpha, -base));
+                sum = exchanged<16>(sum)[0] + exchanged<16>(sum)[1];
+                sum = exchanged<32>(sum)[0] + exchanged<32>(sum)[1];
+                if (lane < 16 && m < M) head.part[(size_t)(2 * tn + wn) * M + m] = make_float2(top, sum);
+                // the target's column among the lane's
+                const int64_t t = target[i] - head.v0 - nw;
+                const int tcol = t >= 0 && t < 16 * NJ && t < N - nw && (((int)t >> 2) & 3) == (lane >> 4) ? (int)t - nsub : -1;
+                if (__ballot(tcol >= 0) != 0) {   // (few rows of few tiles)
+                    float z = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z = tcol == 16 * j + e ? v[j][e] : z;
+                    if (tcol >= 0) head.picked[m] = z * alpha;
                 }
             }
         }
+        if constexpr (HEAD == HEAD_GRAD) {
+            // gradients of the logits over the row's factor, G[m][n]; rows that are ignored and columns beyond N are zero, so that G can be
+            // walked in whole slots as the next product's k
+            const int mw = m0 + wm * 128 + 8 * mrow;          // first of this lane's eight rows
+            const int nl = n0 + wn * 16 * NJ + 2 * nsub;      // first of its columns nl + 32*j + 0..7
+            int tcol[8];
+            bool keep[8], whole = n0 + (wn + 1) * 16 * NJ <= N, hit = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = __float_as_int(row[i].w);
+                keep[i] = t != INT_MIN;
+                whole = whole && keep[i];
+                const int64_t c = (int64_t)t - head.v0 - nl;   // 32*j + 0..7: this lane's
+                tcol[i] = t >= 0 && c >= 0 && c < 16 * NJ && (c & 31) < 8 ? (int)c : -1;
+                hit = hit || tcol[i] >= 0;
+            }
+            // most waves see neither an ignored row, nor an edge, nor a target
+            const bool plain = __ballot(!whole || hit) == 0;
+#pragma unroll
+            for (int jj = 0; jj < NJ; jj += 2) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int n = nl + 16 * jj;
+                float g[8][8];   // [row][column n + c]
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        g[i][c] = row[i].y * __builtin_amdgcn_exp2f(__builtin_fmaf(acc_read(acc[jj + (c >> 2)][i][c & 3]), alpha, -row[i].x));
+                if (!plain) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            if (tcol[i] == 16 * jj + c) g[i][c] -= row[i].z;
+                            if (!keep[i] || n + c >= N) g[i][c] = 0.0f;
+                        }
+                }
+                if (n < head.g_cols)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (mw + i < M)
+                            *reinterpret_cast<uint4*>(head.g + (size_t)(mw + i) * head.ld_g + n) =
+                                make_uint4(pack_bf16x2(g[i][0], g[i][1]), pack_bf16x2(g[i][2], g[i][3]), pack_bf16x2(g[i][4], g[i][5]),
+                                           pack_bf16x2(g[i][6], g[i][7]));
+            }
+        }
+        if constexpr (KNW) {
+            // fp32 sums of the shares of k, rows of ld_sum values; or the result itself, bf16
+            float* const sums = head.sum != nullptr ? head.sum + (size_t)blockIdx.y * M * head.ld_sum : nullptr;
+            if (sums == nullptr)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) times[i] *= head.scale;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int m = m0 + wm * 128 + i * 16 + mrow;
+                if (m >= M) continue;
+                if (sums != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        const int n = n0 + wn * 16 * NJ + j * 16 + nsub;
+                        if (n >= N) continue;
+                        f32x4 c;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) c[e] = acc_read(acc[j][i][e]);
+                        f32x4* const at = reinterpret_cast<f32x4*>(sums + (size_t)m * head.ld_sum + n);   // (rows are padded to four columns)
+                        if (head.add) c += *at;
+                        *at = c;
+                    }
+                    continue;
+                }
+                // rows of 16 lanes swap halves of two blocks: a lane has eight neighbours of one of them, four lanes 64 bytes of a row
+#pragma unroll
+                for (int j = 0; j < NJ; j += 2) {
+                    uint32_t w[2][2];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            w[b][e] = pack_bf16x2(times[i] * acc_read(acc[j + b][i][2 * e]), times[i] * acc_read(acc[j + b][i][2 * e + 1]));
+                    const auto lo = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
+                    const auto hi = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
+                    const uint32_t v[4] = {lo[0], hi[0], lo[1], hi[1]};
+                    const int n = n0 + wn * 16 * NJ + (j + ((lane >> 4) & 1)) * 16 + (lane >> 5) * 8;
+                    uint16_t* const out = C + (size_t)m * head.ld_out + n;
+                    if (n + 7 < N) {
+                        __builtin_memcpy(out, v, 16);   // (one store, whatever the rows' alignment)
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (n + e < N) out[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                    }
+                }
+            }
+        }
+        if (!more) return;
     }
 }
 
@@ -436,7 +471,11 @@ int launch_head_part(int kind, int nj, const void* A, const void* W, void* C, in
     if (rc != ROV_OK) return rc;
     const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + 32 * nj - 1) / (32 * nj);
     if (!grid_fits(tiles_m * tiles_n, 256)) return ROV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
+    // a workgroup a compute unit, whose tiles are a multiple of eight apart, so that they belong to one XCD (with two slots of k or more: a next
+    // tile's first two are loaded during a tile's last two)
+    const long long ncu = device_cu_count() & ~7, tiles = tiles_m * tiles_n;
+    const bool walk = ncu > 0 && tiles > ncu && shares == 1 && K >= 128;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(walk ? ncu : tiles), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
                        (uint16_t*)C, M, N, K, alpha, (int)tiles_m, (int)tiles_n, head);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
