@@ -55,8 +55,19 @@ __global__ __launch_bounds__(256) void xent_stats_kernel(const float* __restrict
     __shared__ float red[4 + 16];
     const int64_t row = blockIdx.x;
     const float* const zr = z + row * cols;
+    // four logits of the row at a time (16 bytes from any address), the last ones one by one
+    auto each = [&](auto take) {
+        const int whole = cols / 4 * 4;
+        for (int c = 4 * threadIdx.x; c < whole; c += 1024) {
+            Piece<float, 4> v;
+            v.load(zr + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) take(scale * v.at(j));
+        }
+        if (whole + (int)threadIdx.x < cols) take(scale * zr[whole + threadIdx.x]);
+    };
     float top = -INFINITY;
-    for (int c = threadIdx.x; c < cols; c += 256) top = fmaxf(top, scale * zr[c]);
+    each([&](float z) { top = fmaxf(top, z); });
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
@@ -67,7 +78,7 @@ __global__ __launch_bounds__(256) void xent_stats_kernel(const float* __restrict
     top = fmaxf(top, st.top);
     const float base = top > -INFINITY ? top : 0.0f;   // (every logit minus infinity: the sum is 0, not NaN)
     float sum = 0.0f;
-    for (int c = threadIdx.x; c < cols; c += 256) sum += __expf(scale * zr[c] - base);
+    each([&](float z) { sum += __expf(z - base); });
     sum = workgroup_sum<256>(sum, red + 4);
     sum += st.sum * __expf(st.top - base);
     if (threadIdx.x != 0) return;
