@@ -125,7 +125,8 @@ __global__ __launch_bounds__(256, 1) void gemm_head_kernel(const char* __restric
         aim_tn = __builtin_amdgcn_readfirstlane(in_band / band_rows);
         aim_m0 = __builtin_amdgcn_readfirstlane(tm * BM);
         aim_n0 = aim_tn * BNT;
-        kstart = __builtin_amdgcn_readfirstlane((int)((unsigned)tm % (unsigned)ns));   // the slot at which the cyclic walk over k starts: tile-rows that run together read W apart
+        // the slot at which the cyclic walk over k starts: tile-rows that run together read W apart
+        kstart = __builtin_amdgcn_readfirstlane((int)((unsigned)tm % (unsigned)ns));
         const int rows_a = M - aim_m0 < BM ? M - aim_m0 : BM;
         const int rows_w = N - aim_n0 < BNT ? N - aim_n0 : BNT;
 #pragma unroll
