@@ -740,10 +740,13 @@ def _ptr(t):
 def norm_residual(x, h, w_pre=None, w_post=None, gate=None, x_scale=1.0, h_scale=1.0, eps=1e-5, y=None, yn=None, yn_fp8_scale=None,
                   stream=None):
     """(y, yn): y = x_scale * x + h_scale * gate * (RMS(h) * w_post), yn = RMS(y) * w_pre (None without w_pre); x, h [..., n],
-    gate [n] or [gates, n] (consecutive rows share a gate).  yn_fp8_scale: yn in e4m3 bytes with that scale."""
+    gate [n] or [gates, n] (consecutive rows share a gate).  yn_fp8_scale (above 0): yn in e4m3 bytes with that scale."""
     shape = x.shape
     if x.numel() == 0 or x.dim() == 0:
         raise ValueError("norm_residual: x must be [..., n], not empty")
+    # (a scale of 0, also one that fp32 rounds to 0, is the library's sign for a result of x's type: twice the bytes that yn has here)
+    if yn_fp8_scale is not None and not ctypes.c_float(yn_fp8_scale).value > 0.0:
+        raise ValueError("norm_residual: yn_fp8_scale must be above 0 in fp32")
     n = shape[-1]
     _on_gpu("norm_residual", x.dtype, ("x", "h", "w_pre", "w_post", "gate", "y"), (x, h, w_pre, w_post, gate, y))
     if y is None:
