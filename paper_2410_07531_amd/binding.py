@@ -610,6 +610,12 @@ def block_forward_static(weights, x, y, cfg, schedule, seed, offset, mask, main_
 # strides go to ctypes packed (bytes are taken as a pointer to them): a quarter of the time of a ctypes array
 _pack4, _pack6, _pack12 = (struct.Struct("%dq" % n).pack for n in (4, 6, 12))
 _torch = _current_device = None
+# sizes go to the library as C ints, and ctypes would keep only their low bits
+_INT_MAX = 0x7FFFFFFF
+
+
+def _refuse_sizes(what):
+    raise RovError(ERR_UNSUPPORTED, what + " (a size beyond 2^31 - 1)")
 
 
 def _start():
@@ -649,6 +655,8 @@ def _on_gpu(what, dtype, names, tensors):
 def make_rope_cfg(rot, theta, layout=ROPE_INTERLEAVED, scaling=ROPE_SCALE_NONE, factor=1.0, turns_low=1.0, turns_high=4.0,
                   trained_len=0, magnitude=1.0):
     """Rotary positions of a head's first `rot` elements (rov_rope_cfg)."""
+    if not (-_INT_MAX <= rot <= _INT_MAX and -_INT_MAX <= trained_len <= _INT_MAX):
+        _refuse_sizes("make_rope_cfg")
     return RopeCfg(layout, rot, scaling, trained_len, theta, factor, turns_low, turns_high, magnitude)
 
 
@@ -656,6 +664,8 @@ def rope(cfg, Q, K=None, positions=None, Qo=None, Ko=None, backward=False, strea
     """Q [B,S,H,d] and K [B,S,Hkv,d] turned by their positions (int64 [B,S], [1,S] or [S]; None: 0..S-1) into
     Qo and Ko (new if None; Q and K themselves for in place).  backward: gradients of Q and K from those of the results."""
     B, S, H, d = shape = Q.shape
+    if (B | S | H | d) > _INT_MAX:
+        _refuse_sizes("rov_rope")
     _on_gpu("rope", Q.dtype, ("Q", "K", "Qo", "Ko"), (Q, K, Qo, Ko))
     if Qo is None:
         Qo = _new_like(Q, stream)
@@ -669,6 +679,8 @@ def rope(cfg, Q, K=None, positions=None, Qo=None, Ko=None, backward=False, strea
         if len(kshape) != 4 or kshape[0] != B or kshape[1] != S or kshape[3] != d:
             raise ValueError("rope: K must be [B, S, Hkv, d] beside Q [B, S, H, d]")
         Hkv = kshape[2]
+        if Hkv > _INT_MAX:
+            _refuse_sizes("rov_rope")
         if Ko is None:
             Ko = _new_like(K, stream)
         elif Ko.shape != kshape:
@@ -748,6 +760,8 @@ def norm_residual(x, h, w_pre=None, w_post=None, gate=None, x_scale=1.0, h_scale
     if yn_fp8_scale is not None and not ctypes.c_float(yn_fp8_scale).value > 0.0:
         raise ValueError("norm_residual: yn_fp8_scale must be above 0 in fp32")
     n = shape[-1]
+    if n > _INT_MAX:
+        _refuse_sizes("rov_norm_residual")
     _on_gpu("norm_residual", x.dtype, ("x", "h", "w_pre", "w_post", "gate", "y"), (x, h, w_pre, w_post, gate, y))
     if y is None:
         y = _new_like(x, stream)
@@ -765,6 +779,8 @@ def norm_residual(x, h, w_pre=None, w_post=None, gate=None, x_scale=1.0, h_scale
 
 
 def norm_residual_bwd_workspace_bytes(rows, n, rows_per_gate, dtype):
+    if n > _INT_MAX:
+        return 0
     return int(load().rov_norm_residual_bwd_workspace_bytes(int(rows), int(n), int(rows_per_gate), int(dtype)))
 
 
@@ -779,6 +795,8 @@ def norm_residual_bwd(y, h, dy, dn=None, w_pre=None, w_post=None, gate=None, x_s
     if like.numel() == 0 or like.dim() == 0:
         raise ValueError("norm_residual_bwd: the gradients must be [..., n], not empty")
     n = shape[-1]
+    if n > _INT_MAX:
+        _refuse_sizes("rov_norm_residual_bwd")
     names, tensors = ("y", "h", "dy", "dn", "dx", "dh"), (y, h, dy, dn, dx, dh)
     _on_gpu("norm_residual_bwd", dt, names + ("w_pre", "w_post", "gate"), tensors + (w_pre, w_post, gate))
     if dx is None:
@@ -806,14 +824,18 @@ def norm_residual_bwd(y, h, dy, dn=None, w_pre=None, w_post=None, gate=None, x_s
 
 
 def linear_xent_workspace_bytes(M, V, K, dtype, backward=False, vocab_piece=0):
+    if max(M, V, K, vocab_piece) > _INT_MAX:
+        return 0
     return int(load().rov_linear_xent_workspace_bytes(int(M), int(V), int(K), int(dtype), int(bool(backward)), int(vocab_piece)))
 
 
-def _xent_operands(what, X, W, targets, f32, outs):
+def _xent_operands(what, X, W, targets, f32, outs, vocab_piece):
     """Checks what both calls take; (M, V, K, row strides of X, W and the results)."""
     if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[1]:
         raise ValueError("%s: X must be [M, K] and W [V, K]" % what)
     (M, K), V = X.shape, W.shape[0]
+    if (M | V | K) > _INT_MAX or vocab_piece > _INT_MAX:
+        _refuse_sizes("rov_" + what)
     _on_gpu(what, X.dtype, ("X", "W", "dX", "dW"), (X, W) + outs)
     _on_gpu(what, _torch.int64, ("targets",), (targets,))
     _on_gpu(what, _torch.float32, tuple(f32), tuple(f32.values()))
@@ -834,7 +856,7 @@ def _xent_workspace(what, workspace, X, stream, *sizes):
 
 def linear_xent(X, W, targets, scale=1.0, ignore_index=-100, loss=None, lse=None, vocab_piece=0, workspace=None, stream=None):
     """(loss, lse), fp32 [M], of the logits scale * X @ W^T (X [M, K], W [V, K]) against targets (int64 [M])."""
-    M, V, K, ldx, ldw, _, _ = _xent_operands("linear_xent", X, W, targets, dict(loss=loss, lse=lse), ())
+    M, V, K, ldx, ldw, _, _ = _xent_operands("linear_xent", X, W, targets, dict(loss=loss, lse=lse), (), vocab_piece)
     if loss is None:
         loss = _new((M,), X, stream, _torch.float32)
     if lse is None:
@@ -850,7 +872,7 @@ def linear_xent(X, W, targets, scale=1.0, ignore_index=-100, loss=None, lse=None
 def linear_xent_bwd(X, W, targets, lse, dloss, dlse=None, scale=1.0, ignore_index=-100, dX=None, dW=None, need_dX=True, need_dW=True,
                     vocab_piece=0, workspace=None, stream=None):
     """(dX, dW) from linear_xent's lse and the gradients of loss and lse (fp32 [M]); None for one that is not needed."""
-    M, V, K, ldx, ldw, lddx, lddw = _xent_operands("linear_xent_bwd", X, W, targets, dict(lse=lse, dloss=dloss, dlse=dlse), (dX, dW))
+    M, V, K, ldx, ldw, lddx, lddw = _xent_operands("linear_xent_bwd", X, W, targets, dict(lse=lse, dloss=dloss, dlse=dlse), (dX, dW), vocab_piece)
     if dX is None and need_dX:
         dX = _new((M, K), X, stream, X.dtype)
     if dW is None and need_dW:

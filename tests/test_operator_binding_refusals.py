@@ -13,3 +13,48 @@ def test_a_scale_of_zero_does_not_ask_for_two_bytes_an_element(scale, given):
     yn = torch.zeros(4, 64, dtype=torch.uint8) if given else None
     with pytest.raises(ValueError, match="yn_fp8_scale"):
         rov.norm_residual(x, x, w_pre=w, yn=yn, yn_fp8_scale=scale)
+
+
+class _NotAsked:
+    def __getattr__(self, name):
+        raise AssertionError("%s was asked with sizes that a C int does not hold" % name)
+
+
+BIG = 2 ** 32 + 8      # a C int would hold 8
+
+
+def _calls_with_big_sizes():
+    t = lambda *shape, dtype=torch.bfloat16: torch.empty(*shape, dtype=dtype, device="meta")   # (no memory behind them)
+    cfg = rov.make_rope_cfg(8, 1e4)
+    for at in range(4):
+        shape = [1, 2, 2, 8]
+        shape[at] = BIG
+        yield "rope %d" % at, lambda shape=shape: rov.rope(cfg, t(*shape))
+    yield "rope keys", lambda: rov.rope(cfg, t(1, 2, 2, 8), t(1, 2, BIG, 8))
+    yield "rope form", lambda: rov.make_rope_cfg(BIG, 1e4)
+    yield "rope form, trained length", lambda: rov.make_rope_cfg(8, 1e4, trained_len=BIG)
+    yield "norm", lambda: rov.norm_residual(t(1, BIG), t(1, BIG))
+    yield "norm back", lambda: rov.norm_residual_bwd(None, None, t(1, BIG))
+    for M, V, K, piece in ((BIG, 4, 8, 0), (4, BIG, 8, 0), (4, 4, BIG, 0), (4, 4, 8, BIG)):
+        args = (t(M, K), t(V, K), t(M, dtype=torch.int64))
+        f = t(M, dtype=torch.float32)
+        yield "loss %d %d %d %d" % (M, V, K, piece), lambda args=args, piece=piece: rov.linear_xent(*args, vocab_piece=piece)
+        yield "loss back %d %d %d %d" % (M, V, K, piece), lambda args=args, f=f, piece=piece: rov.linear_xent_bwd(*args, f, f, vocab_piece=piece)
+
+
+@pytest.mark.parametrize("name,call", list(_calls_with_big_sizes()), ids=lambda v: v.replace(" ", "_") if isinstance(v, str) else "")
+def test_sizes_that_a_c_int_does_not_hold(monkeypatch, name, call):
+    monkeypatch.setattr(rov, "_on_gpu", lambda *a: None)
+    monkeypatch.setattr(rov, "_torch", torch)
+    monkeypatch.setattr(rov, "load", lambda: _NotAsked())
+    monkeypatch.setattr(rov, "_stream_ptr", lambda stream: 0)
+    with pytest.raises(rov.RovError) as e:
+        call()
+    assert e.value.code == rov.ERR_UNSUPPORTED
+
+
+def test_workspaces_of_sizes_that_a_c_int_does_not_hold():
+    for sizes in ((BIG, 10, 8), (4, BIG, 8), (4, 10, BIG)):
+        assert rov.linear_xent_workspace_bytes(*sizes, rov.BF16) == 0
+    assert rov.linear_xent_workspace_bytes(4, 10, 8, rov.BF16, True, BIG) == 0
+    assert rov.norm_residual_bwd_workspace_bytes(8, BIG, 8, rov.BF16) == 0
