@@ -253,14 +253,15 @@ __global__ __launch_bounds__(NT, VPT * W <= 8 ? 4 : 1) void norm_bwd_kernel(cons
         keep(kept_post, (const T*)p.w_post);
     }
     int parity = 0;
-    for (int group = WHOLE ? (int)blockIdx.x : (int)blockIdx.x / p.chunks; group < p.groups; group += WHOLE ? (int)gridDim.x : p.groups) {
-        int64_t r0 = (int64_t)group * p.rows_per_gate, r1 = r0 + p.rows_per_gate;
+    // (64 bits: the step behind the last of 2^31 - 1 groups)
+    for (int64_t group = WHOLE ? (int)blockIdx.x : (int)blockIdx.x / p.chunks; group < p.groups; group += WHOLE ? (int)gridDim.x : p.groups) {
+        int64_t r0 = group * p.rows_per_gate, r1 = r0 + p.rows_per_gate;
         if constexpr (!WHOLE) {
             const int64_t len = p.rows_per_gate, chunk = (int)blockIdx.x % p.chunks;
             r1 = r0 + len * (chunk + 1) / p.chunks;
             r0 += len * chunk / p.chunks;
         }
-        const T* const gate = p.gate != nullptr ? (const T*)p.gate + (int64_t)group * p.n : nullptr;
+        const T* const gate = p.gate != nullptr ? (const T*)p.gate + group * p.n : nullptr;
         if constexpr (AHEAD) keep(kept_gate, gate);
         Row cur, next;
         if (AHEAD && r0 < r1) fetch(next, r0);
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(NT, VPT * W <= 8 ? 4 : 1) void norm_bwd_kernel(cons
                 load_or<RAGGED, T, W>(gate, e, p.n, g, 1.0f);
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    if (p.dgate != nullptr && (!RAGGED || e + j < p.n)) p.dgate[(int64_t)group * p.n + e + j] = p.h_scale * wp[j] * col_h[c][j];
+                    if (p.dgate != nullptr && (!RAGGED || e + j < p.n)) p.dgate[group * p.n + e + j] = p.h_scale * wp[j] * col_h[c][j];
                     col_g[c][j] = __builtin_fmaf(g[j], col_h[c][j], col_g[c][j]);
                     col_h[c][j] = 0.0f;
                 }
