@@ -321,7 +321,7 @@ __global__ __launch_bounds__(NT, VPT * W <= 8 ? 4 : 1) void norm_bwd_kernel(cons
                     col_y[c][j] = __builtin_fmaf(dn * r, y, col_y[c][j]);
                     col_h[c][j] = __builtin_fmaf(gy * rh, h, col_h[c][j]);
                     dx[j] = p.x_scale * gy;
-                    dh[j] = rh * wp.at(j) * (p.h_scale * g.at(j) * gy) - h * mh;
+                    dh[j] = rh * wp.at(j) * (p.h_scale * g.at(j) * gy) - (has_post ? h * mh : 0.0f);   // (h may be infinite: times mh = 0 it would be NaN)
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 Piece<T, W> out;
