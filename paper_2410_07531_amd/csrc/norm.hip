@@ -8,7 +8,7 @@
 //     dgate = sum over the gate's rows of h_scale g P(h).
 // What bounds both: memory (4 and 6 passes over rows x n).  A workgroup holds a row in registers, so each tensor
 // passes once (backward, rows of more than 1024 pieces are read twice); all sums are fp32 in a fixed order.
-// 16384 x 4096 in bf16, both norms: 90 us; 8192 x 8192 backward: 171 us, 4.7 TB/s; 4096 x 16384 backward: 400 us, two vector passes over it.
+// 16384 x 4096 in bf16, both norms: 90 us; 8192 x 8192 backward: 171 us, 4.7 TB/s; 4096 x 16384 backward: 370 us, two vector passes over it.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -305,8 +305,10 @@ __global__ __launch_bounds__(NT, VPT * W <= 8 ? 4 : 1) void norm_bwd_kernel(cons
             parity ^= 1;
             const float r = has_pre ? 1.0f / sqrtf(sum[0] * p.inv_n + p.eps) : 0.0f;
             const float rh = has_post ? 1.0f / sqrtf(sum[2] * p.inv_n + p.eps) : 1.0f;
-            const float my = has_pre ? r * r * r * sum[1] * p.inv_n : 0.0f;     // y times this is hat * r * mean(hat t)
-            const float mh = has_post ? rh * rh * rh * p.inv_n * p.h_scale * (sum[3] + r * sum[4] - my * sum[5]) : 0.0f;
+            // means of hat t and of (h r_h) w_post q.  Each factor r goes to an element or a sum of its row, never r * r alone, so that everything
+            // between is of the size of results (the cube of r leaves fp32 for rows beyond 1e13, or 1e-13 with a tiny eps)
+            const float my = has_pre ? r * sum[1] * p.inv_n : 0.0f;
+            const float mh = has_post ? rh * (sum[3] + r * sum[4] - r * sum[5] * (r * my)) * p.inv_n * p.h_scale : 0.0f;
 #pragma unroll
             for (int c = 0; c < VPT; ++c) {
                 const int e = (c * NT + (int)threadIdx.x) * W;
@@ -317,11 +319,13 @@ __global__ __launch_bounds__(NT, VPT * W <= 8 ? 4 : 1) void norm_bwd_kernel(cons
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
                     const float y = now.y.at(j), h = now.h.at(j), dn = now.dn.at(j);
-                    const float gy = now.dy.at(j) + r * w.at(j) * dn - y * my;
-                    col_y[c][j] = __builtin_fmaf(dn * r, y, col_y[c][j]);
-                    col_h[c][j] = __builtin_fmaf(gy * rh, h, col_h[c][j]);
+                    const float hat = y * r, hat_h = h * rh;
+                    const float gy = now.dy.at(j) + r * (w.at(j) * dn - hat * my);
+                    col_y[c][j] = __builtin_fmaf(dn, hat, col_y[c][j]);
+                    col_h[c][j] = __builtin_fmaf(gy, hat_h, col_h[c][j]);
                     dx[j] = p.x_scale * gy;
-                    dh[j] = rh * wp.at(j) * (p.h_scale * g.at(j) * gy) - (has_post ? h * mh : 0.0f);   // (h may be infinite: times mh = 0 it would be NaN)
+                    // (without w_post h may be infinite: times mh = 0 it would be NaN)
+                    dh[j] = rh * (wp.at(j) * (p.h_scale * g.at(j) * gy) - (has_post ? hat_h * mh : 0.0f));
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 Piece<T, W> out;

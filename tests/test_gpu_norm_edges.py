@@ -62,3 +62,35 @@ def test_without_a_norm_behind_the_branch_its_gradient_does_not_depend_on_it(dty
     near(dh, 0.5 * spread * gy, 0.5 * mag * (spread.abs() if gated else 1.0), dtype)
     if gated:
         near(dgate, (0.5 * gy * h.double()).view(2, 3, n).sum(1), (0.5 * mag * h.double().abs()).view(2, 3, n).sum(1), "f32", 2.0 ** -16)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [72, 100, 1030, 9000])
+@pytest.mark.parametrize("size,eps", [(1e13, 1e-5), (1e15, 1e-5), (1e17, 1e-5), (1e-13, 1e-28), (1e-15, 1e-32), (0.0, 1e-30)])
+def test_rows_far_from_one_and_rows_of_zeros(dtype, n, size, eps):
+    # dx and dh are of the size of dn / size (dn is sent in that large, so that they are of the size of one) and each is a difference of two
+    # terms as large as it: hat's and h_hat's means must not vanish, nor 0 times a factor beyond fp32 become NaN.  Branch and stream lean on their
+    # gradients, so that the means are 0.3 to 0.7 and not near 0.
+    rows, f64 = 4, torch.float64
+    g = torch.Generator().manual_seed(n + 1)
+    r = lambda *s: torch.randn(*s, generator=g)
+    to = lambda v: v.to(DT[dtype]).cuda()
+    dn, q0 = r(rows, n), r(rows, n)
+    gain = size if size else 1.0
+    y, h = to(size * (0.5 * dn + r(rows, n))), to(size * (0.5 * q0 + r(rows, n)))
+    w_pre, w_post, gate = to(1 + 0.1 * r(n)), to(1 + 0.1 * r(n)), to(0.5 + 0.1 * r(n))
+    dn, dy = to(gain * dn), to(q0)
+    dx, dh, dw_pre, dw_post, dgate = rov.norm_residual_bwd(y, h, dy, dn, w_pre, w_post, gate, h_scale=0.5, eps=eps)
+    Y, H, DN, DY, WN, WP, GT = (v.to(f64) for v in (y, h, dn, dy, w_pre, w_post, gate))
+    mean = lambda v: v.mean(1, keepdim=True)
+    ry, rh = 1 / torch.sqrt(mean(Y * Y) + eps), 1 / torch.sqrt(mean(H * H) + eps)
+    hat, hh, t = Y * ry, H * rh, WN * DN
+    if size:
+        assert float((mean(hat * t) / gain).abs().min()) > 0.1
+    gy, my = DY + ry * (t - hat * mean(hat * t)), DY.abs() + ry * (t.abs() + hat.abs() * mean((hat * t).abs()))
+    q, mq = 0.5 * GT * gy * WP, 0.5 * (GT * WP).abs() * my
+    near(dx, gy, my, dtype)
+    near(dh, rh * (q - hh * mean(hh * q)), rh * (mq + hh.abs() * mean(hh.abs() * mq)), dtype)
+    near(dw_pre, (DN * hat).sum(0), (DN * hat).abs().sum(0), "f32", 2.0 ** -16)
+    near(dw_post, (0.5 * GT * gy * hh).sum(0), (0.5 * GT.abs() * my * hh.abs()).sum(0), "f32", 2.0 ** -16)
+    near(dgate, (0.5 * WP * gy * hh).sum(0), (0.5 * WP.abs() * my * hh.abs()).sum(0), "f32", 2.0 ** -16)
