@@ -715,6 +715,7 @@ extern "C" int rov_linear_xent_bwd(const void* X, const void* W, const int64_t* 
     using namespace rov;
     ROV_STEP(check_xent(X, W, targets, M, V, K, ldx, ldw, dtype, scale, ignore_index, vocab_piece));
     if (lse == nullptr || dloss == nullptr || dX == dW) return ROV_ERR_INVALID;
+    if ((dX != nullptr && dX == W) || (dW != nullptr && dW == X)) return ROV_ERR_INVALID;   // (the next piece of the vocabulary reads both operands)
     if (!aligned(lse, 4) || !aligned(dloss, 4) || !aligned(dlse, 4)) return ROV_ERR_INVALID;
     const size_t esz = dtype == ROV_F32 ? 4 : 2;
     if ((dX != nullptr && (lddx < K || !aligned(dX, esz))) || (dW != nullptr && (lddw < K || !aligned(dW, esz)))) return ROV_ERR_INVALID;

@@ -58,3 +58,12 @@ def test_workspaces_of_sizes_that_a_c_int_does_not_hold():
         assert rov.linear_xent_workspace_bytes(*sizes, rov.BF16) == 0
     assert rov.linear_xent_workspace_bytes(4, 10, 8, rov.BF16, True, BIG) == 0
     assert rov.norm_residual_bwd_workspace_bytes(8, BIG, 8, rov.BF16) == 0
+
+
+@pytest.mark.parametrize("dtype", [rov.BF16, rov.F32])
+def test_gradients_over_the_other_operand_are_refused_by_the_library(dtype):
+    # pointers that are never followed: one piece's gradients over an operand that the next piece reads
+    X, W, dX, dW = 4096, 8192, 12288, 16384
+    call = lambda dX, dW: rov.load().rov_linear_xent_bwd(X, W, 4096, 4096, 4096, None, 8, 8, 8, 8, 8, dtype, 1.0, -100, dX, dW, 8, 8, 0, 4096, 0, None)
+    assert call(dX, dW) == rov.ERR_WORKSPACE        # (nothing else is wrong with the call)
+    assert call(W, dW) == call(dX, X) == call(W, X) == call(W, None) == call(None, X) == rov.ERR_INVALID
