@@ -635,6 +635,9 @@ int rov_block_forward_opts(const rov_block_weights *w, const rov_block_opts *opt
  * bf16 operands are reached by 32-bit offsets: 256 rows of X or W, and for the gradients M rows of K or of a piece, must stay below
  * 4 GiB, else ROV_ERR_UNSUPPORTED. */
 size_t rov_linear_xent_workspace_bytes(int M, int V, int K, int dtype, int backward, int vocab_piece);
+/* The products of a bf16 call of these sizes, operands on 16 bytes, that have more tiles than compute units, so that a workgroup takes one tile
+ * after the other: 1 the loss's logits (backward == 0); 2 the gradients' logits, 4 dX, 8 dW, of any piece (backward != 0); or an error. */
+int rov_linear_xent_walks(int M, int V, int K, int backward, int vocab_piece);
 int rov_linear_xent(const void *X, const void *W, const int64_t *targets, int M, int V, int K, int64_t ldx,
                     int64_t ldw, int dtype, float scale, int64_t ignore_index, float *loss, float *lse,
                     int vocab_piece, void *workspace, size_t workspace_bytes, void *stream);

@@ -135,6 +135,7 @@ SIGNATURES = {
     "rov_norm_residual_bwd_workspace_bytes": (ctypes.c_size_t, [_i64, _i, _i64, _i]),
     "rov_norm_residual_bwd": (_i, [_p] * 12 + [_i64, _i, _p, _i64, _i, _f, _f, _f, _p, ctypes.c_size_t, _p]),
     "rov_linear_xent_workspace_bytes": (ctypes.c_size_t, [_i] * 6),
+    "rov_linear_xent_walks": (_i, [_i] * 5),
     "rov_linear_xent": (_i, [_p, _p, _p, _i, _i, _i, _i64, _i64, _i, _f, _i64, _p, _p, _i, _p, ctypes.c_size_t, _p]),
     "rov_linear_xent_bwd": (_i, [_p] * 6 + [_i, _i, _i, _i64, _i64, _i, _f, _i64, _p, _p, _i64, _i64, _i, _p, ctypes.c_size_t, _p]),
 }
@@ -827,6 +828,14 @@ def linear_xent_workspace_bytes(M, V, K, dtype, backward=False, vocab_piece=0):
     if max(M, V, K, vocab_piece) > _INT_MAX:
         return 0
     return int(load().rov_linear_xent_workspace_bytes(int(M), int(V), int(K), int(dtype), int(bool(backward)), int(vocab_piece)))
+
+
+def linear_xent_walks(M, V, K, backward=False, vocab_piece=0):
+    """The products of a bf16 call whose workgroups take several tiles: 1 logits of the loss, 2 logits of the gradients, 4 dX, 8 dW."""
+    r = load().rov_linear_xent_walks(M, V, K, int(bool(backward)), vocab_piece)
+    if r < 0:
+        raise RovError(r, "rov_linear_xent_walks")
+    return r
 
 
 def _xent_operands(what, X, W, targets, f32, outs, vocab_piece):

@@ -459,6 +459,11 @@ __global__ __launch_bounds__(256, 1) void gemm_head_kernel(const char* __restric
     }
 }
 
+// A workgroup a compute unit, whose tiles are a multiple of eight apart, so that they belong to one XCD (with two slots of k or more: a next
+// tile's first two are loaded during a tile's last two)?  Else a workgroup a tile.
+long long walkers() { return device_cu_count() & ~7; }
+bool walks(long long tiles, int K, int shares) { return walkers() > 0 && tiles > walkers() && shares == 1 && K >= 128; }
+
 int launch_head_part(int kind, int nj, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
                      hipStream_t stream) {
     const bool ragged = kind <= HEAD_GRAD && K % 64 != 0;
@@ -472,11 +477,8 @@ int launch_head_part(int kind, int nj, const void* A, const void* W, void* C, in
     if (rc != ROV_OK) return rc;
     const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + 32 * nj - 1) / (32 * nj);
     if (!grid_fits(tiles_m * tiles_n, 256)) return ROV_ERR_UNSUPPORTED;
-    // a workgroup a compute unit, whose tiles are a multiple of eight apart, so that they belong to one XCD (with two slots of k or more: a next
-    // tile's first two are loaded during a tile's last two)
-    const long long ncu = device_cu_count() & ~7, tiles = tiles_m * tiles_n;
-    const bool walk = ncu > 0 && tiles > ncu && shares == 1 && K >= 128;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(walk ? ncu : tiles), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
+    const long long tiles = tiles_m * tiles_n;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(walks(tiles, K, shares) ? walkers() : tiles), (unsigned)shares), dim3(256), kLdsBytes, stream, (const char*)A, (const char*)W,
                        (uint16_t*)C, M, N, K, alpha, (int)tiles_m, (int)tiles_n, head);
     ROV_LAUNCH_CHECK();
     return ROV_OK;
@@ -489,7 +491,21 @@ long long wide_lines(long long lines, long long across) {
     const long long ncu = device_cu_count(), full = lines * across / ncu * ncu / across;
     return 2 * across * (lines - full) <= ncu ? full : lines;
 }
+// Of M x N: the columns (HEAD_STATS, HEAD_GRAD) or rows (HEAD_DX, HEAD_DW) that run as 256 x 256 tiles.
+long long wide_part(bool kn, int M, int N, int shares) {
+    const long long tiles_m = ((long long)M + BM - 1) / BM, tiles_n = ((long long)N + BN - 1) / BN;
+    return !kn ? wide_lines(tiles_n, tiles_m) * BN : shares > 1 ? M : wide_lines(tiles_m, tiles_n) * BM;
+}
 }  // namespace
+
+bool gemm_head_walks(int kind, int M, int N, int K, int shares) {
+    const bool kn = kind == HEAD_DX || kind == HEAD_DW;
+    const long long all = kn ? M : N, part = wide_part(kn, M, N, shares), wide = part < all ? part : all, rest = all - wide;
+    auto tiles = [&](long long along, int width) {
+        return kn ? (along + BM - 1) / BM * (((long long)N + width - 1) / width) : ((long long)M + BM - 1) / BM * ((along + width - 1) / width);
+    };
+    return walks(tiles(wide, BN), K, shares) || walks(tiles(rest, BN / 2), K, shares);
+}
 
 int gemm_head_parts(int M, int N) {
     const long long lines = (N + BN - 1) / BN, wide = wide_lines(lines, (M + BM - 1) / BM);
@@ -508,10 +524,10 @@ int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int
     if ((unsigned long long)(kna ? slots * 64 : BM) * head.ld_a + 1024 > 0xFFFFFFFFull ||
         (unsigned long long)(kn ? slots * 64 : BN) * head.ld_w + 1024 > 0xFFFFFFFFull)
         return ROV_ERR_UNSUPPORTED;
-    const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
     HeadArgs h = head;
+    const long long part = wide_part(kn, M, N, shares);
     if (!kn) {   // columns beyond the full rounds: narrower tiles
-        const int wide = (int)(wide_lines(tiles_n, tiles_m) * BN);
+        const int wide = part < N ? (int)part : N;
         if (wide >= N) return launch_head_part(kind, 8, A, W, C, M, N, K, alpha, 1, head, stream);
         if (wide > 0) {
             h.g_cols = wide;
@@ -524,7 +540,7 @@ int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int
         if (h.part != nullptr) h.part += (size_t)(wide / 128) * M;
         return launch_head_part(kind, 4, A, (const char*)W + (size_t)wide * head.ld_w, C, M, N - wide, K, alpha, 1, h, stream);
     }
-    const int wide = shares > 1 ? M : (int)(wide_lines(tiles_m, tiles_n) * BM);   // rows
+    const int wide = part < M ? (int)part : M;   // rows
     if (wide >= M) return launch_head_part(kind, 8, A, W, C, M, N, K, alpha, shares, head, stream);
     if (wide > 0) {
         const int rc = launch_head_part(kind, 8, A, W, C, wide, N, K, alpha, 1, head, stream);

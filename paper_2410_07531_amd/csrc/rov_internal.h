@@ -136,6 +136,7 @@ struct HeadArgs {
     bool add = false;
 };
 int gemm_head_parts(int M, int N);
+bool gemm_head_walks(int kind, int M, int N, int K, int shares);   // does a workgroup take several tiles?
 int launch_gemm_head(int kind, const void* A, const void* W, void* C, int M, int N, int K, float alpha, int shares, const HeadArgs& head,
                      hipStream_t stream);
 

@@ -649,6 +649,24 @@ int head_backward(const void* X, const void* W, const int64_t* targets, const fl
     return dX != nullptr && sum_x != nullptr ? fold(sum_x, l.shares_x, l.ks, dX, lddx, M, K, h.factor, 1, scale, st) : ROV_OK;
 }
 
+// The products of head_forward and head_backward whose workgroups take several tiles, for operands that lie as the kernels take them.
+int head_walks(int M, int V, int K, const HeadLayout& l, bool backward) {
+    const int kx = (int)l.kp, piece = K % 8 != 0 ? l.packed : backward ? l.piece : V;
+    int found = 0;
+    for (int v0 = 0; v0 < V; v0 += piece) {
+        const int cols = V - v0 < piece ? V - v0 : piece;
+        if (!backward) {
+            found |= gemm_head_walks(HEAD_STATS, M, cols, kx, 1) ? 1 : 0;
+            continue;
+        }
+        const int64_t slots = up_to(cols, 64) / 64;
+        found |= gemm_head_walks(HEAD_GRAD, M, cols, kx, 1) ? 2 : 0;
+        found |= gemm_head_walks(HEAD_DX, M, K, cols, l.shares_x > slots ? (int)slots : l.shares_x) ? 4 : 0;
+        found |= M > 128 && gemm_head_walks(HEAD_DW, cols, K, M, l.shares_w) ? 8 : 0;
+    }
+    return found;
+}
+
 int copy(const void* src, int64_t lds, void* dst, int64_t ldd, int64_t rows, int cols, const int64_t* targets, int64_t ignore, hipStream_t st) {
     hipLaunchKernelGGL(xent_copy_kernel, dim3(sweep_grid(rows * cols)), dim3(256), 0, st, (const float*)src, lds, (float*)dst, ldd, rows, cols, targets,
                        ignore);
@@ -670,6 +688,14 @@ bool dense(const void* p, int64_t ld, int K) { return ld == K && aligned(p, 16);
 extern "C" size_t rov_linear_xent_workspace_bytes(int M, int V, int K, int dtype, int backward, int vocab_piece) {
     if (M <= 0 || V <= 0 || K <= 0 || vocab_piece < 0 || (dtype != ROV_F32 && dtype != ROV_BF16)) return 0;
     return dtype == ROV_BF16 ? rov::head_layout(M, V, K, vocab_piece, backward != 0).total : rov::layout(M, V, K, vocab_piece, backward != 0).total;
+}
+
+extern "C" int rov_linear_xent_walks(int M, int V, int K, int backward, int vocab_piece) {
+    if (M <= 0 || V <= 0 || K <= 0 || vocab_piece < 0) return ROV_ERR_INVALID;
+    using namespace rov;
+    const HeadLayout l = head_layout(M, V, K, vocab_piece, backward != 0);
+    ROV_STEP(check_head(M, V, K, K, l, backward != 0));
+    return head_walks(M, V, K, l, backward != 0);
 }
 
 extern "C" int rov_linear_xent(const void* X, const void* W, const int64_t* targets, int M, int V, int K, int64_t ldx, int64_t ldw, int dtype,

@@ -1,5 +1,5 @@
-"""Loss over the vocabulary with softmaxes that are not one-hot, and the proof on the CPU that the comparison would
-show a wrong tile.
+"""Loss over the vocabulary with softmaxes that are not one-hot, at sizes where a workgroup takes one tile or several, and the proof on the CPU
+that the comparison would show a wrong tile.
 
 Inputs: rows of W of length S, X normal plus the multiple of the target's row that adds LEAN to its logit, so that a row's logits spread by about S
 and its target has a probability around a half of what LEAN makes of it: from 0.02 to 0.9 over the rows.
@@ -19,8 +19,20 @@ from paper_2410_07531_amd import binding as rov
 gpu = pytest.mark.gpu
 S = 1.5
 
+# rows, vocabulary, K, columns of a piece, products whose workgroups take several tiles (loss, gradients): 1 and 2 logits, 4 dX, 8 dW
+WALKS = [(300, 51000, 128, 0, 1, 2),        # two slots of k: the next tile is aimed at in the first
+         (600, 34000, 192, 0, 1, 2),        # three slots
+         (300, 51000, 136, 0, 1, 2),        # the last slot a part
+         (300, 51000, 264, 0, 1, 2 | 8),
+         (130, 51000, 264, 0, 0, 8),        # dW over two slots and a part
+         (500, 51000, 300, 0, 1, 2 | 8),    # packed operands
+         (1000, 33200, 264, 0, 1, 2),       # two full rounds of tiles and a rest of narrower ones
+         (150, 66000, 264, 0, 0, 8),        # the same for dW
+         (51000, 300, 264, 0, 1, 2 | 4),    # dX at once
+         (51000, 600, 264, 256, 1, 4),      # dX summed over pieces
+         (66000, 300, 512, 0, 1, 2 | 4)]    # rows: full rounds and a rest
 PLAIN = [s for s in L.SIZES if s[1] >= 200]
-CASES = PLAIN
+CASES = PLAIN + [s[:4] for s in WALKS]
 
 
 def make(M, V, K, dtype, seed=0, ignored=0.2):
@@ -134,3 +146,32 @@ def test_rows_with_one_gradient_or_none(dtype):
     L.close(dX, r["dX"], r["tX"], "dX")
     L.close(dW, r["dW"], r["tW"], "dW")
     assert bool((dX[1::10] == 0).all())
+
+
+def test_which_products_walk_over_tiles():
+    # (256 compute units: the chip's, and what the library goes by without one)
+    for M, V, K, piece, forward, backward in WALKS:
+        assert rov.linear_xent_walks(M, V, K, False, piece) == forward and rov.linear_xent_walks(M, V, K, True, piece) == backward, (M, V, K, piece)
+    assert rov.linear_xent_walks(8192, 131072, 4096, True) == 2 | 4 | 8
+    for M, V, K, piece in L.SIZES:      # those of the other tests have a tile a workgroup
+        assert rov.linear_xent_walks(M, V, K, False, piece) == rov.linear_xent_walks(M, V, K, True, piece) == 0
+    for bad in ((0, 10, 8), (4, -1, 8), (4, 10, 0)):
+        with pytest.raises(rov.RovError) as e:
+            rov.linear_xent_walks(*bad)
+        assert e.value.code == rov.ERR_INVALID
+
+
+@gpu
+@pytest.mark.parametrize("M,V,K,piece,forward,backward", WALKS)
+def test_a_workgroup_with_several_tiles(M, V, K, piece, forward, backward):
+    print("xent walk", M, V, K, piece, flush=True)
+    assert rov.linear_xent_walks(M, V, K, False, piece) == forward and rov.linear_xent_walks(M, V, K, True, piece) == backward
+    X, W, t, dloss = (v.cuda() for v in make(M, V, K, "bf16"))
+    r = answer(X, W, t, dloss)[0]
+    loss, lse = rov.linear_xent(X, W, t, vocab_piece=piece)
+    dX, dW = rov.linear_xent_bwd(X, W, t, lse, dloss, vocab_piece=piece)
+    assert faults(r, loss, lse, dX, dW, M) == []
+    for _ in range(3):      # the same bits each time, whatever ran before
+        rov.linear_xent_bwd(X.flip(0), W, t, lse, dloss, vocab_piece=piece)
+        again = rov.linear_xent(X, W, t, vocab_piece=piece) + rov.linear_xent_bwd(X, W, t, lse, dloss, vocab_piece=piece)
+        assert all(torch.equal(a, b) for a, b in zip(again, (loss, lse, dX, dW)))
