@@ -579,7 +579,7 @@ int rov_rope(const rov_rope_cfg *cfg, const void *Q, void *Qo, const void *K, vo
  * is formed from y before y is rounded.  yn_fp8_scale > 0 (bf16 only): yn holds OCP e4m3 bytes of
  * (value / yn_fp8_scale), as the fp8 products take their activations; else 0.
  * ld: row strides of x, h, y, yn in elements (>= n).  y and yn may be x or h (with the same stride; e4m3 yn may not), not each other.
- * n > 32768: ROV_ERR_UNSUPPORTED. */
+ * n > 32768, or more rows than a launch has workgroups (4194303 of more than 512 16-byte pieces, more of shorter ones): ROV_ERR_UNSUPPORTED. */
 int rov_norm_residual(const void *x, const void *h, const void *w_post, const void *gate, const void *w_pre,
                       void *y, void *yn, int64_t rows, int n, const int64_t ld[4], int64_t rows_per_gate, int dtype,
                       float x_scale, float h_scale, float eps, float yn_fp8_scale, void *stream);

@@ -545,7 +545,7 @@ int check_norm_residual(const void* x, const void* h, const void* w_post, const 
     for (int i = 0; i < 2; ++i)
         for (int o = 0; o < 2; ++o)
             if (outs[o] == ins[i] && ld[2 + o] != ld[i] && rows > 1) return ROV_ERR_INVALID;
-    return ROV_OK;
+    return grid_fits(rows, row_shape(n, dtype).nt) ? ROV_OK : ROV_ERR_UNSUPPORTED;   // (a workgroup a row)
 }
 
 int launch_norm_residual(const void* x, const void* h, const void* w_post, const void* gate, const void* w_pre, void* y, void* yn,
@@ -560,7 +560,6 @@ int launch_norm_residual(const void* x, const void* h, const void* w_post, const
     NormParams p{x, h, w_post, gate, w_pre, y, yn, ld[0], ld[1], ld[2], ld[3], (int)rows, n, (int)rows_per_gate,
                  x_scale, h_scale, eps, 1.0f / (float)n, out8 ? 1.0f / yn_fp8_scale : 1.0f};
     const RowShape shape = row_shape(n, dtype);
-    if (!grid_fits(rows, shape.nt)) return ROV_ERR_UNSUPPORTED;
     if (dtype == ROV_F32) launch_fwd<float, false>(p, shape, stream);
     else if (out8) launch_fwd<uint16_t, true>(p, shape, stream);
     else launch_fwd<uint16_t, false>(p, shape, stream);

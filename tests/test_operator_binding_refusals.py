@@ -1,4 +1,6 @@
 """What the binding of the operators around the block refuses by itself, before the library or a device is asked (no GPU needed)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -67,3 +69,14 @@ def test_gradients_over_the_other_operand_are_refused_by_the_library(dtype):
     call = lambda dX, dW: rov.load().rov_linear_xent_bwd(X, W, 4096, 4096, 4096, None, 8, 8, 8, 8, 8, dtype, 1.0, -100, dX, dW, 8, 8, 0, 4096, 0, None)
     assert call(dX, dW) == rov.ERR_WORKSPACE        # (nothing else is wrong with the call)
     assert call(W, dW) == call(dX, X) == call(W, X) == call(W, None) == call(None, X) == rov.ERR_INVALID
+
+
+def test_a_block_whose_norms_have_too_many_rows_is_refused_before_anything_runs():
+    # 4.2 million tokens of 4160 values are more workgroups than a launch of the norm behind the branch has; pointers are never followed
+    P, hidden = 1 << 20, 4160
+    cfg = rov.make_block_cfg(1, 1, 64, hidden, 64, 0.0)
+    w = rov.BlockWeights(*[P] * 7, (ctypes.c_float * 5)(*[1.0] * 5))
+    opts = rov.BlockOpts(None, None, 0, P, None, None, None, 0, 1.0, 1.0)
+    call = lambda B: rov.load().rov_block_forward_opts(ctypes.byref(w), ctypes.byref(opts), P, 2 * P, B, 129, ctypes.byref(cfg), rov.SCHED_FUSED, 1, 0, 0, None, None,
+                                                       P, 1 << 62, None, None)
+    assert call(1 << 15) == rov.ERR_UNSUPPORTED
