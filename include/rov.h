@@ -630,8 +630,9 @@ int rov_block_forward_opts(const rov_block_weights *w, const rov_block_opts *opt
  * lie outside [0, V)) has loss 0 and no gradient, whatever its X holds; any other target outside [0, V) gives a NaN loss (and NaN gradients).
  * scale > 0.  dtype of X and W: ROV_F32 or ROV_BF16; row strides ldx, ldw >= K in elements.  Logits and sums are fp32.
  * vocab_piece: columns of a piece (rounded up to 256), 0: chosen by the library; it sets the workspace's size and
- * does not change what is computed beyond the order of fp32 sums.
- * workspace: 256-byte aligned device scratch of rov_linear_xent_workspace_bytes (0 for invalid arguments).
+ * does not change what is computed beyond the order of fp32 sums.  The bf16 loss keeps no piece of anything: it ignores vocab_piece.
+ * workspace: 256-byte aligned device scratch of rov_linear_xent_workspace_bytes (0 for invalid arguments), which is enough for operands of
+ * any stride and address (bf16: room for a packed X and up to 128 MiB of packed W).
  * bf16 operands are reached by 32-bit offsets: 256 rows of X or W, and for the gradients M rows of K or of a piece, must stay below
  * 4 GiB, else ROV_ERR_UNSUPPORTED. */
 size_t rov_linear_xent_workspace_bytes(int M, int V, int K, int dtype, int backward, int vocab_piece);

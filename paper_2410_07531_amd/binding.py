@@ -864,7 +864,8 @@ def _xent_workspace(what, workspace, X, stream, *sizes):
 
 
 def linear_xent(X, W, targets, scale=1.0, ignore_index=-100, loss=None, lse=None, vocab_piece=0, workspace=None, stream=None):
-    """(loss, lse), fp32 [M], of the logits scale * X @ W^T (X [M, K], W [V, K]) against targets (int64 [M])."""
+    """(loss, lse), fp32 [M], of the logits scale * X @ W^T (X [M, K], W [V, K]) against targets (int64 [M]).  vocab_piece: fp32 only (the bf16
+    loss keeps no piece of the logits)."""
     M, V, K, ldx, ldw, _, _ = _xent_operands("linear_xent", X, W, targets, dict(loss=loss, lse=lse), (), vocab_piece)
     if loss is None:
         loss = _new((M,), X, stream, _torch.float32)

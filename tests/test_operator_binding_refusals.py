@@ -80,3 +80,11 @@ def test_a_block_whose_norms_have_too_many_rows_is_refused_before_anything_runs(
     call = lambda B: rov.load().rov_block_forward_opts(ctypes.byref(w), ctypes.byref(opts), P, 2 * P, B, 129, ctypes.byref(cfg), rov.SCHED_FUSED, 1, 0, 0, None, None,
                                                        P, 1 << 62, None, None)
     assert call(1 << 15) == rov.ERR_UNSUPPORTED
+
+
+def test_what_the_piece_of_the_vocabulary_sets():
+    # the bf16 loss keeps no logits: its workspace does not depend on the piece; fp32's does, and both gradients'
+    size = lambda dtype, backward, piece: rov.linear_xent_workspace_bytes(512, 60000, 256, dtype, backward, piece)
+    assert size(rov.BF16, False, 0) == size(rov.BF16, False, 1024) == size(rov.BF16, False, 60000) > 0
+    for dtype, backward in ((rov.F32, False), (rov.F32, True), (rov.BF16, True)):
+        assert 0 < size(dtype, backward, 1024) < size(dtype, backward, 60000)
