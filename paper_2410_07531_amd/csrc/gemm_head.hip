@@ -9,9 +9,9 @@
 //   - HEAD_DX: the second operand lies as [K, N] (rows of k), HEAD_DW: both do.  Such an operand's part of a slot is 64 rows of k by the
 //     tile's columns; fragments come by the transposing LDS load, two a fragment, with the k order of the other operand's.
 //   - a workgroup takes one tile after the other, and the loads of a tile's last two slots' time are the next tile's first: its loop goes on
-//     behind the epilogue as if there were one longer k.  Against a tile a workgroup, us: loss with gradients 1000 x 50257 x 1024 502 / 487, 8192 x
-//     50257 x 1024 3160 / 3046, 4096 x 50304 x 256 770 / 730, 8192 x 131072 x 4096 26050 / 25910; loss alone 2048 x 131072 x 4096 1600 / 1574.  What
-//     the epilogue reads is asked for before the loop, and no wait stands before its stores: loads sent out between loop and epilogue gained nothing.
+//     behind the epilogue as if there were one longer k.  A tile a workgroup / this, in turn on one box, us: loss with gradients 1000 x 50257 x 1024
+//     500 / 488, 8192 x 50257 x 1024 3017 / 2990, 4096 x 50304 x 256 775 / 727, 8192 x 131072 x 4096 24990 / 24800; loss alone 2048 x 131072 x 4096
+//     1549 / 1523.  What the epilogue reads is asked for before the loop, and no wait stands before its stores: loads sent out between loop and epilogue gained nothing.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
