@@ -28,6 +28,7 @@ WALKS = [(300, 51000, 128, 0, 1, 2),        # two slots of k: the next tile is a
          (500, 51000, 300, 0, 1, 2 | 8),    # packed operands
          (1000, 33200, 264, 0, 1, 2),       # two full rounds of tiles and a rest of narrower ones
          (150, 66000, 264, 0, 0, 8),        # the same for dW
+         (16, 131073, 136, 0, 1, 2),        # few rows, whose dW has a kernel of its own
          (51000, 300, 264, 0, 1, 2 | 4),    # dX at once
          (51000, 600, 264, 256, 1, 4),      # dX summed over pieces
          (66000, 300, 512, 0, 1, 2 | 4)]    # rows: full rounds and a rest
@@ -175,3 +176,34 @@ def test_a_workgroup_with_several_tiles(M, V, K, piece, forward, backward):
         rov.linear_xent_bwd(X.flip(0), W, t, lse, dloss, vocab_piece=piece)
         again = rov.linear_xent(X, W, t, vocab_piece=piece) + rov.linear_xent_bwd(X, W, t, lse, dloss, vocab_piece=piece)
         assert all(torch.equal(a, b) for a, b in zip(again, (loss, lse, dX, dW)))
+
+
+@gpu
+def test_several_tiles_captured_and_beside_another_call():
+    # a graph replayed between eager calls, and two streams that work on different inputs at once, each with its own workspace
+    M, V, K = 300, 51000, 264
+    X, W, t, dloss = (v.cuda() for v in make(M, V, K, "bf16"))
+    X2, t2 = X.flip(0).contiguous(), t.flip(0).contiguous()
+
+    def both(X, t, stream=None):
+        loss, lse = rov.linear_xent(X, W, t, stream=stream)
+        return (loss, lse) + rov.linear_xent_bwd(X, W, t, lse, dloss, stream=stream)
+
+    want, want2 = both(X, t), both(X2, t2)
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        a, b = both(X, t, one), both(X2, t2, two)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(a + b, want + want2))
+    held, at = X.clone(), t.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both(held, at)
+    for x, y, w in ((X2, t2, want2), (X, t, want), (X2, t2, want2)):
+        held.copy_(x)
+        at.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(got, w))
+        assert all(torch.equal(u, v) for u, v in zip(both(X, t), want))
