@@ -1,4 +1,4 @@
-"""What the binding of the operators around the block refuses by itself, before the library or a device is asked (no GPU needed)."""
+"""What the operators around the block refuse on the host, in the binding and in the library, and what their workspaces go by (no GPU needed)."""
 import ctypes
 
 import pytest
